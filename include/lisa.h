@@ -47,10 +47,12 @@ typedef enum lisa_status_t {
     LISA_ERR_UNSUPPORTED = 2, /* well-formed but outside the supported ranges above */
     LISA_ERR_WORKSPACE = 3,   /* workspace missing or smaller than lisa_workspace_bytes() */
     LISA_ERR_CUDA = 4,        /* a CUDA call failed; the code is kept for lisa_last_cuda_error() */
-    LISA_ERR_TIMEOUT = 5      /* a bounded device-side wait ran out (reported by lisa_check) */
+    LISA_ERR_TIMEOUT = 5,     /* a bounded device-side wait ran out (reported by lisa_check) */
+    LISA_ERR_NO_PAGES = 6     /* lisa_pages_reserve found fewer free pages than it needed (reported by lisa_check) */
 } lisa_status_t;
 
-typedef enum lisa_dtype_t { LISA_F32 = 0, LISA_BF16 = 1 } lisa_dtype_t;
+/* S8 and E4M3 are the code types of paged caches (see lisa_paged_layer) and appear nowhere else. */
+typedef enum lisa_dtype_t { LISA_F32 = 0, LISA_BF16 = 1, LISA_S8 = 2, LISA_E4M3 = 3 } lisa_dtype_t;
 typedef enum lisa_act_t { LISA_ACT_NONE = 0, LISA_ACT_RELU = 1, LISA_ACT_SILU = 2 } lisa_act_t;
 
 /* Eq. 4's Integrate.  ADD: A_n = FFN(A_{n-1}) + A_Delta.  CONCAT (Sec. 5.1, "An overview of LiSA"):
@@ -61,7 +63,7 @@ typedef enum lisa_integrate_t { LISA_INTEGRATE_ADD = 0, LISA_INTEGRATE_CONCAT = 
 typedef enum lisa_cache_kind_t { LISA_CACHE_STANDARD = 0, LISA_CACHE_SHARED = 1 } lisa_cache_kind_t;
 typedef enum lisa_op_t {
     LISA_OP_ANCHOR = 0, LISA_OP_SHARED_PREFILL = 1, LISA_OP_SHARED_DECODE = 2, LISA_OP_SHARED_PREFILL_CHAIN = 3,
-    LISA_OP_SHARED_PREFILL_CARRY = 4
+    LISA_OP_SHARED_PREFILL_CARRY = 4, LISA_OP_ANCHOR_PAGED = 5, LISA_OP_SHARED_DECODE_PAGED = 6
 } lisa_op_t;
 
 /* A strided view of an activation tensor [B, N, H, x]; x contiguous. */
@@ -340,6 +342,143 @@ lisa_status_t lisa_kvcache_append(const lisa_kvcache_layer* layer, const lisa_te
 lisa_status_t lisa_kvcache_append_layer(const lisa_kvcache* cache, int32_t layer, const lisa_tensor* k_or_kp, const lisa_tensor* v,
                                         const int32_t* seq_lens_before, int32_t n_new, lisa_stream_t stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Paged 8-bit cache.  A layer's cache is a pool of pages of page_tokens positions (16, 32, 64 or 128), for all KV heads; sequence b's
+ * position j lies in page table[b][j / page_tokens].  Values are held as 8-bit codes with a scale for every block of
+ * LISA_PAGE_BLOCK positions and head: value = code * scale, a code being an int8 in -127..127 (LISA_S8, scale = amax / 127) or an e4m3
+ * (LISA_E4M3, scale = amax / 448).  A page's bytes, in order (lisa_paged_layout_of gives the offsets):
+ *   K codes  STANDARD [Hkv][page_tokens][d];  SHARED: K' [Hkv][page_tokens / 16][r][16]; padded to 128 bytes
+ *   V codes  [Hkv][page_tokens][d]
+ *   scales   [Hkv][page_tokens / 16][2] fp32: K's (or K''s) and V's; the page is padded to 128 bytes
+ * Memory is the caller's, 128-byte aligned: n_pages * page_bytes bytes a layer.  Nothing in it has to be set before its first append.
+ * A table entry outside 0..n_pages-1 where a position is read or written is not followed: the position counts as absent, and
+ * lisa_check() then reports LISA_ERR_INVALID_ARG.  Entries behind a sequence's length are never read. */
+#define LISA_PAGE_BLOCK 16
+typedef struct lisa_paged_layer {
+    int32_t kind;        /* lisa_cache_kind_t */
+    int32_t dtype;       /* LISA_S8 or LISA_E4M3 */
+    int32_t Hkv;
+    int32_t d;
+    int32_t r;           /* SHARED only */
+    int32_t page_tokens; /* 16, 32, 64 or 128 */
+    int32_t n_pages;
+    int32_t reserved;
+    void* pages;         /* device */
+} lisa_paged_layer;
+typedef struct lisa_paged_layout {
+    size_t v_offset, scale_offset, page_bytes;
+} lisa_paged_layout;
+lisa_status_t lisa_paged_layout_of(const lisa_paged_layer* layer, lisa_paged_layout* layout); /* host-only; `pages` is not read */
+
+/* The page tables of a call's B sequences: row b starts at pages + b * stride (elements). */
+typedef struct lisa_page_table {
+    const int32_t* pages; /* device int32 */
+    int64_t stride;
+    int32_t B;
+    int32_t max_pages;    /* entries of a row */
+} lisa_page_table;
+
+/* Writing rows into a paged layer, and reading them back.
+ * append: rows first[b] .. first[b] + counts[b] - 1 of sequence b are quantised from k_or_kp [B,n,Hkv,d|r] and v [B,n,Hkv,d] (rows
+ *   0 .. counts[b]-1 of them).  The scale of a block is its largest magnitude over 127 (448); where the block already holds positions before
+ *   first[b] the larger of that and its present scale, and if that grows it, what the block holds is rescaled to it.  Rounding is to nearest even
+ *   of x / scale in fp32.  A block that is given a value that is not finite gets the scale NaN (until it is written from its start again), which every reader then sees: the error is
+ *   not hidden.  Positions at or beyond max_pages * page_tokens, or on an invalid page, are dropped and counted (lisa_check).
+ * read: rows first[b] .. first[b] + counts[b] - 1 are written, dequantised, to rows 0.. of k_or_kp and v; rows beyond counts[b], and absent ones, are left as they are.
+ * first (device int32 [B]): NULL = 0.  counts (device int32 [B]; clamped to 0..n): NULL = n.  V and STANDARD K rows must be 16-byte
+ * aligned (strides too), K' to its type.  k_or_kp and v have one type, fp32 or bf16.  A page that two rows of the table share is written by both: see lisa_pages_reserve. */
+typedef struct lisa_paged_rows_args {
+    size_t struct_size;
+    int32_t B, n;
+    const lisa_paged_layer* layer;
+    lisa_page_table table;
+    lisa_tensor k_or_kp, v;
+    const int32_t* first;
+    const int32_t* counts;
+} lisa_paged_rows_args;
+lisa_status_t lisa_paged_append(const lisa_paged_rows_args* args, lisa_stream_t stream);
+lisa_status_t lisa_paged_read(const lisa_paged_rows_args* args, lisa_stream_t stream);
+
+/* lisa_attn_anchor's decode step against a STANDARD paged layer: q [B,1,Hq,d], o the same, score rows as there.  Sequence b has
+ * seq_lens[b] positions (device int32 [B], clamped to 0..L) or L when that is NULL; L <= max_pages * page_tokens.  A sequence without positions
+ * (length 0) gets o = 0.  Codes enter the products as they are and every sum is fp32; scores are what fp32 arithmetic gives for the cached values.
+ * Workspace: lisa_workspace_bytes(LISA_OP_ANCHOR_PAGED, args, &n); a buffer sized for the largest B and L serves every smaller step. */
+typedef struct lisa_paged_anchor_args {
+    size_t struct_size;
+    int32_t B, Hq, L;
+    int32_t scores_dtype; /* lisa_dtype_t of out_scores: LISA_F32 or LISA_BF16 */
+    lisa_tensor q, o;
+    const lisa_paged_layer* cache;
+    lisa_page_table table;
+    const int32_t* seq_lens;
+    void* out_scores;     /* [B, Hq, >= length] or NULL */
+    int64_t scores_stride_b, scores_stride_h;
+    void* workspace;
+    size_t workspace_bytes;
+} lisa_paged_anchor_args;
+lisa_status_t lisa_attn_anchor_paged(const lisa_paged_anchor_args* args, lisa_stream_t stream);
+
+/* lisa_attn_shared_decode against a SHARED paged layer: same link, score rows and results, the cached K' and V being the codes' values.
+ * Lengths, table, absent positions and workspace (LISA_OP_SHARED_DECODE_PAGED) as for lisa_attn_anchor_paged. */
+typedef struct lisa_paged_shared_args {
+    size_t struct_size;
+    int32_t B, Hq, L;
+    int32_t scores_dtype; /* lisa_dtype_t of prev_scores AND out_scores */
+    const void* prev_scores;
+    int64_t prev_stride_b, prev_stride_h;
+    lisa_link link;
+    const lisa_paged_layer* cache;
+    lisa_page_table table;
+    const int32_t* seq_lens;
+    lisa_tensor o;
+    void* out_scores;     /* may be NULL, must not alias prev_scores */
+    int64_t scores_stride_b, scores_stride_h;
+    void* workspace;
+    size_t workspace_bytes;
+} lisa_paged_shared_args;
+lisa_status_t lisa_attn_shared_decode_paged(const lisa_paged_shared_args* args, lisa_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * The bookkeeping of pages: which sequence holds which.  All of it lives on the device, in the caller's memory, so that a serving loop
+ * needs no copy to the host: B rows of page ids (-1: none), their lengths, and for every page how many table entries name it (0: free).
+ * A page id names that page in every layer's pool.  Results do not depend on the order in which threads run.
+ *   table  [B] rows of max_pages entries; row b's first ceil(lens[b] / page_tokens) entries (or more, where reserved) are its pages
+ *   work   lisa_pages_work_bytes() bytes of scratch
+ * 1 <= B <= LISA_MAX_PAGE_ROWS. */
+#define LISA_MAX_PAGE_ROWS 1024
+typedef struct lisa_pages {
+    size_t struct_size;
+    int32_t B, max_pages, n_pages, page_tokens;
+    int64_t table_stride; /* elements */
+    int32_t* table;
+    int32_t* lens;
+    int32_t* refs;        /* [n_pages] */
+    void* work;
+    size_t work_bytes;
+} lisa_pages;
+lisa_status_t lisa_pages_work_bytes(const lisa_pages* pages, size_t* bytes); /* host-only */
+
+/* Row i takes over the pages and the length of row parent[i] (device int32 [B]); parent[i] == i keeps its own, parent[i] == -1 frees it (any other
+ * value outside 0..B-1 too, and is counted for lisa_check).  All rows change at once, so parent may be a permutation.  Nothing is copied:
+ * the pages are shared until someone writes (lisa_pages_reserve). */
+lisa_status_t lisa_pages_fork(const lisa_pages* pages, const int32_t* parent, lisa_stream_t stream);
+
+/* Gives row b the pages for new positions lens[b] .. lens[b] + n_new[b] - 1 (device int32 [B]; NULL: one each; negative counts as 0): row by row,
+ * the lowest free page first.  A partly filled page that other entries name too is exchanged for a copy, in every layer; if nobody but writers holds
+ * it, the last of them keeps it.  lens is not changed.  If the free pages do not suffice, or a row would outgrow max_pages, nothing is changed at
+ * all and lisa_check() reports LISA_ERR_NO_PAGES. */
+lisa_status_t lisa_pages_reserve(const lisa_pages* pages, const lisa_paged_layer* layers, int32_t n_layers, const int32_t* n_new,
+                                 lisa_stream_t stream);
+
+/* Moves the pages in use to the front of the pool: of u pages in use those at u or beyond go to the free ones below u, both in ascending order,
+ * in every layer; table and refs follow. */
+lisa_status_t lisa_pages_compact(const lisa_pages* pages, const lisa_paged_layer* layers, int32_t n_layers, lisa_stream_t stream);
+
+/* Copies page src[i] to dst[i] in every layer, i < n (device int32 [n]).  No dst may be among the src or twice among the dst; pairs with an id
+ * outside a pool are skipped and counted (lisa_check). */
+lisa_status_t lisa_pages_copy(const lisa_paged_layer* layers, int32_t n_layers, const int32_t* src, const int32_t* dst, int32_t n,
+                              lisa_stream_t stream);
+
 /* Host-only helpers (no device work). */
 
 /* Bytes of the one buffer that backs every layer of `desc` (each k and v rounded up to 256 bytes), and the carving of
@@ -355,8 +494,8 @@ lisa_status_t lisa_kvcache_bytes(const lisa_kvcache_layer* layer, size_t* k_byte
 lisa_status_t lisa_workspace_bytes(int32_t op, const void* args, size_t* bytes);
 
 /* Synchronises `stream` and reports device-side conditions recorded since the last call: a dropped cache
- * append (LISA_ERR_INVALID_ARG) or a bounded wait that ran out (LISA_ERR_TIMEOUT); LISA_ERR_CUDA if the
- * stream itself reports an error. */
+ * append or a page id out of range (LISA_ERR_INVALID_ARG), a bounded wait that ran out (LISA_ERR_TIMEOUT) or a lack of free pages
+ * (LISA_ERR_NO_PAGES); LISA_ERR_CUDA if the stream itself reports an error. */
 lisa_status_t lisa_check(lisa_stream_t stream);
 
 int lisa_last_cuda_error(void);             /* the cudaError_t of the last LISA_ERR_CUDA on this thread, else 0 */

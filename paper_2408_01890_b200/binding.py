@@ -18,12 +18,13 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblisa_b200.so")
 
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
-F32, BF16 = 0, 1
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_NO_PAGES = range(7)
+F32, BF16, S8, E4M3 = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 INTEGRATE_ADD, INTEGRATE_CONCAT, INTEGRATE_PLUS = 0, 1, 2
 CACHE_STANDARD, CACHE_SHARED = 0, 1
 OP_ANCHOR, OP_SHARED_PREFILL, OP_SHARED_DECODE, OP_SHARED_PREFILL_CHAIN, OP_SHARED_PREFILL_CARRY = 0, 1, 2, 3, 4
+OP_ANCHOR_PAGED, OP_SHARED_DECODE_PAGED = 5, 6
 ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU}
 
 # include/lisa.h (the method's entry points and host helpers) and include/lisa_debug.h (test and measurement hooks)
@@ -31,11 +32,15 @@ EXPORTS = ["lisa_attn_anchor", "lisa_attn_shared_prefill", "lisa_attn_shared_pre
            "lisa_attn_shared_prefill_carry", "lisa_prefill_scores_bytes", "lisa_attn_shared_prefill_carry_host",
            "lisa_carry_host_arena_bytes",
            "lisa_host_arena_bytes", "lisa_attn_shared_decode", "lisa_attn_shared_decode_static", "lisa_kvcache_append",
+           "lisa_paged_layout_of", "lisa_paged_append", "lisa_paged_read", "lisa_attn_anchor_paged", "lisa_attn_shared_decode_paged",
+           "lisa_pages_work_bytes", "lisa_pages_fork", "lisa_pages_reserve", "lisa_pages_compact", "lisa_pages_copy",
            "lisa_kvcache_append_layer", "lisa_project", "lisa_kvcache_bytes", "lisa_kvcache_total_bytes", "lisa_kvcache_init",
            "lisa_workspace_bytes", "lisa_check", "lisa_last_cuda_error", "lisa_status_string", "lisa_version",
            "lisa_prefill_phase_times", "lisa_prefill_phase_timing", "lisa_force_general_kernels", "lisa_kernel_launches",
            "lisa_debug_wait_timeout"]
 MAX_LAYERS = 128
+PAGE_BLOCK = 16         # positions of a paged cache that share a scale
+MAX_PAGE_ROWS = 1024
 
 
 class LisaError(RuntimeError):
@@ -113,6 +118,45 @@ class SharedDecodeArgs(C.Structure):
                 ("scores_stride_h", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class CPagedLayer(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("dtype", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("r", C.c_int32),
+                ("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("reserved", C.c_int32), ("pages", C.c_void_p)]
+
+
+class CPagedLayout(C.Structure):
+    _fields_ = [("v_offset", C.c_size_t), ("scale_offset", C.c_size_t), ("page_bytes", C.c_size_t)]
+
+
+class CPageTable(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("stride", C.c_int64), ("B", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class PagedRowsArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("B", C.c_int32), ("n", C.c_int32), ("layer", C.POINTER(CPagedLayer)), ("table", CPageTable),
+                ("k_or_kp", Tensor), ("v", Tensor), ("first", C.c_void_p), ("counts", C.c_void_p)]
+
+
+class PagedAnchorArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("B", C.c_int32), ("Hq", C.c_int32), ("L", C.c_int32), ("scores_dtype", C.c_int32),
+                ("q", Tensor), ("o", Tensor), ("cache", C.POINTER(CPagedLayer)), ("table", CPageTable), ("seq_lens", C.c_void_p),
+                ("out_scores", C.c_void_p), ("scores_stride_b", C.c_int64), ("scores_stride_h", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class PagedSharedArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("B", C.c_int32), ("Hq", C.c_int32), ("L", C.c_int32), ("scores_dtype", C.c_int32),
+                ("prev_scores", C.c_void_p), ("prev_stride_b", C.c_int64), ("prev_stride_h", C.c_int64), ("link", CLink),
+                ("cache", C.POINTER(CPagedLayer)), ("table", CPageTable), ("seq_lens", C.c_void_p), ("o", Tensor),
+                ("out_scores", C.c_void_p), ("scores_stride_b", C.c_int64), ("scores_stride_h", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class CPages(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("B", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("table_stride", C.c_int64), ("table", C.c_void_p), ("lens", C.c_void_p), ("refs", C.c_void_p), ("work", C.c_void_p),
+                ("work_bytes", C.c_size_t)]
+
+
 _lib = None
 _ext = None
 
@@ -158,9 +202,20 @@ def load():
         lib.lisa_check.argtypes = [C.c_void_p]
         lib.lisa_kernel_launches.restype = C.c_uint64
         lib.lisa_debug_wait_timeout.argtypes = [C.c_int64, C.c_void_p]
+        lib.lisa_paged_layout_of.argtypes = [C.POINTER(CPagedLayer), C.POINTER(CPagedLayout)]
+        lib.lisa_paged_append.argtypes = [C.POINTER(PagedRowsArgs), C.c_void_p]
+        lib.lisa_paged_read.argtypes = [C.POINTER(PagedRowsArgs), C.c_void_p]
+        lib.lisa_attn_anchor_paged.argtypes = [C.POINTER(PagedAnchorArgs), C.c_void_p]
+        lib.lisa_attn_shared_decode_paged.argtypes = [C.POINTER(PagedSharedArgs), C.c_void_p]
+        lib.lisa_pages_work_bytes.argtypes = [C.POINTER(CPages), C.POINTER(C.c_size_t)]
+        lib.lisa_pages_fork.argtypes = [C.POINTER(CPages), C.c_void_p, C.c_void_p]
+        lib.lisa_pages_reserve.argtypes = [C.POINTER(CPages), C.POINTER(CPagedLayer), C.c_int32, C.c_void_p, C.c_void_p]
+        lib.lisa_pages_compact.argtypes = [C.POINTER(CPages), C.POINTER(CPagedLayer), C.c_int32, C.c_void_p]
+        lib.lisa_pages_copy.argtypes = [C.POINTER(CPagedLayer), C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
         ext.bind(*[C.cast(getattr(lib, n), C.c_void_p).value for n in (
             "lisa_attn_anchor", "lisa_attn_shared_prefill", "lisa_attn_shared_prefill_carry", "lisa_attn_shared_decode",
-            "lisa_kvcache_append", "lisa_kvcache_append_layer", "lisa_project", "lisa_workspace_bytes")])
+            "lisa_kvcache_append", "lisa_kvcache_append_layer", "lisa_project", "lisa_workspace_bytes", "lisa_paged_append", "lisa_paged_read",
+            "lisa_attn_anchor_paged", "lisa_attn_shared_decode_paged", "lisa_pages_fork", "lisa_pages_reserve", "lisa_pages_compact")])
         _lib, _ext = lib, ext
     return _lib
 
@@ -504,6 +559,139 @@ def lisa_attn_shared_decode_static(prev_scores: torch.Tensor, link: Link, cache:
         a.out_scores, a.scores_stride_b, a.scores_stride_h = out_scores.data_ptr(), out_scores.stride(0), out_scores.stride(1)
     _check(load().lisa_attn_shared_decode_static(C.byref(a), _stream()), "lisa_attn_shared_decode_static")
     return out
+
+
+# ------------------------------------------------------------------ paged 8-bit cache
+class PagedLayer:
+    """One layer of a paged 8-bit cache: `pool`, uint8 [n_pages, page_bytes] (given, or made for n_pages), for all KV heads.
+
+    k, v and scales are views of it: the codes (int8, or float8_e4m3fn) as [n_pages, Hkv, page_tokens, d], for K' of a SHARED layer
+    [n_pages, Hkv, page_tokens / 16, r, 16], and the scales of K (or K') and V, fp32 [n_pages, Hkv, page_tokens / 16, 2]."""
+
+    def __init__(self, kind: int, Hkv: int, page_tokens: int, d: int, r: int = 0, *, dtype: int = S8, n_pages: int = 0,
+                 pool: Optional[torch.Tensor] = None, device="cuda"):
+        self.kind, self.Hkv, self.page_tokens, self.d, self.r, self.dtype = kind, Hkv, page_tokens, d, r, dtype
+        self.n_pages = n_pages if pool is None else int(pool.shape[0])
+        self.desc = CPagedLayer(kind, dtype, Hkv, d, r, page_tokens, self.n_pages, 0, None)
+        lay = CPagedLayout()
+        _check(load().lisa_paged_layout_of(C.byref(self.desc), C.byref(lay)), "lisa_paged_layout_of")
+        self.layout = lay
+        if pool is None:
+            pool = torch.empty((self.n_pages, lay.page_bytes), dtype=torch.uint8, device=device)
+        assert pool.dtype == torch.uint8 and pool.dim() == 2 and pool.shape[1] == lay.page_bytes and pool.is_contiguous() and pool.is_cuda, \
+            "expected a contiguous CUDA pool of bytes [n_pages, %d]" % lay.page_bytes
+        self.pool, self.desc.pages = pool, pool.data_ptr()
+        codes, blocks = torch.int8 if dtype == S8 else torch.float8_e4m3fn, page_tokens // PAGE_BLOCK
+        kw = r if kind == CACHE_SHARED else d
+        self.k = pool[:, :Hkv * page_tokens * kw].view(codes).unflatten(
+            1, (Hkv, blocks, r, PAGE_BLOCK) if kind == CACHE_SHARED else (Hkv, page_tokens, d))
+        self.v = pool[:, lay.v_offset:lay.scale_offset].view(codes).unflatten(1, (Hkv, page_tokens, d))
+        self.scales = pool[:, lay.scale_offset:lay.scale_offset + Hkv * blocks * 8].view(torch.float32).unflatten(1, (Hkv, blocks, 2))
+
+
+class PagedCache:
+    """The paged layers of a stack, which share page ids: kinds[l] is CACHE_STANDARD or CACHE_SHARED.  layers[l] is what the attention calls take."""
+
+    def __init__(self, kinds: Sequence[int], n_pages: int, Hkv: int, page_tokens: int, d: int, r: int = 0, *, dtype: int = S8, device="cuda"):
+        self._set([PagedLayer(k, Hkv, page_tokens, d, r if k == CACHE_SHARED else 0, dtype=dtype, n_pages=n_pages, device=device) for k in kinds])
+
+    @classmethod
+    def of(cls, layers: Sequence[PagedLayer]) -> "PagedCache":
+        self = cls.__new__(cls)
+        self._set(list(layers))
+        return self
+
+    def _set(self, layers):
+        self.layers = layers
+        self.descs = (CPagedLayer * len(layers))(*[l.desc for l in layers])
+
+
+class Pages:
+    """Which sequence holds which pages, all on the device: table [B, max_pages] (-1: none), lens [B], refs [n_pages] (table entries that
+    name a page), int32.  Given tensors are used as they are; Pages.empty makes those of a pool nobody uses."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, page_tokens: int):
+        B = table.shape[0]
+        for x in (table, lens, refs):
+            assert x.dtype == torch.int32 and x.is_cuda and x.stride(-1) == 1, "expected contiguous int32 CUDA tensors"
+        assert table.dim() == 2 and lens.shape == (B,) and refs.dim() == 1
+        self.table, self.lens, self.refs, self.page_tokens = table, lens, refs, page_tokens
+        self.desc = CPages(C.sizeof(CPages), B, table.shape[1], refs.shape[0], page_tokens, table.stride(0), table.data_ptr(), lens.data_ptr(),
+                           refs.data_ptr(), None, 0)
+        n = C.c_size_t()
+        _check(load().lisa_pages_work_bytes(C.byref(self.desc), C.byref(n)), "lisa_pages_work_bytes")
+        self.work = torch.empty(n.value, dtype=torch.uint8, device=table.device)
+        self.desc.work, self.desc.work_bytes = self.work.data_ptr(), n.value
+
+    @classmethod
+    def empty(cls, B: int, max_pages: int, n_pages: int, page_tokens: int, device="cuda") -> "Pages":
+        return cls(torch.full((B, max_pages), -1, dtype=torch.int32, device=device), torch.zeros(B, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device), page_tokens)
+
+
+def lisa_paged_append(layer: PagedLayer, table: torch.Tensor, k_or_kp: torch.Tensor, v: torch.Tensor,
+                      first: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None) -> None:
+    """Rows 0 .. counts[b]-1 (all when None) of k_or_kp [B,n,Hkv,d|r] and v [B,n,Hkv,d] become positions first[b].. (0 when None)."""
+    _check(_native().paged_append(C.addressof(layer.desc), table, k_or_kp, v, first, counts), "lisa_paged_append")
+
+
+def lisa_paged_read(layer: PagedLayer, table: torch.Tensor, first: Optional[torch.Tensor], k_or_kp: torch.Tensor, v: torch.Tensor,
+                    counts: Optional[torch.Tensor] = None) -> None:
+    """Positions first[b] .. first[b]+counts[b]-1, dequantised, into rows 0.. of k_or_kp [B,n,Hkv,d|r] and v [B,n,Hkv,d]."""
+    _check(_native().paged_read(C.addressof(layer.desc), table, k_or_kp, v, first, counts), "lisa_paged_read")
+
+
+def paged_decode_workspace(layer: PagedLayer, B: int, Hq: int, L: int) -> Optional[torch.Tensor]:
+    """Scratch of decode calls on this layer for up to B sequences of up to L positions."""
+    shared = layer.kind == CACHE_SHARED
+    a = PagedSharedArgs() if shared else PagedAnchorArgs()
+    a.struct_size = C.sizeof(a)
+    a.B, a.Hq, a.L = B, Hq, L
+    a.cache = C.pointer(layer.desc)
+    return _workspace(OP_SHARED_DECODE_PAGED if shared else OP_ANCHOR_PAGED, a)
+
+
+def lisa_attn_anchor_paged(q: torch.Tensor, layer: PagedLayer, table: torch.Tensor, *, L: int, seq_lens: Optional[torch.Tensor] = None,
+                           out: Optional[torch.Tensor] = None, out_scores: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A new token's attention over a STANDARD paged layer: q [B,1,Hq,d], lengths seq_lens[b] <= L (L when None)."""
+    out = torch.empty_like(q) if out is None else out
+    _check(_native().anchor_paged(q, C.addressof(layer.desc), table, int(L), seq_lens, out, out_scores, workspace), "lisa_attn_anchor_paged")
+    return out
+
+
+def lisa_attn_shared_decode_paged(prev_scores: torch.Tensor, link: Link, layer: PagedLayer, table: torch.Tensor, *, L: int,
+                                  seq_lens: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                                  out_scores: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """lisa_attn_shared_decode against a SHARED paged layer; returns o [B,1,Hq,d], of Q''s type unless `out` is given."""
+    if out is None:
+        B, _, Hq, _ = link.qp.shape
+        out = torch.empty((B, 1, Hq, layer.d), dtype=link.qp.dtype, device=link.qp.device)
+    _check(_native().shared_paged(prev_scores, link, C.addressof(layer.desc), table, int(L), seq_lens, out, out_scores, workspace),
+           "lisa_attn_shared_decode_paged")
+    return out
+
+
+def lisa_pages_fork(pages: Pages, parent: torch.Tensor) -> None:
+    """Row i takes over the pages and length of row parent[i]; -1 frees it.  parent: int32 [B] on the device."""
+    _check(_native().pages_fork(C.addressof(pages.desc), parent), "lisa_pages_fork")
+
+
+def lisa_pages_reserve(pages: Pages, cache: PagedCache, n_new: Optional[torch.Tensor] = None) -> None:
+    """Pages for n_new[b] (one when None) positions behind lens[b]; shared pages that would be written to are exchanged for copies."""
+    _check(_native().pages_reserve(C.addressof(pages.desc), C.addressof(cache.descs), len(cache.layers), n_new), "lisa_pages_reserve")
+
+
+def lisa_pages_compact(pages: Pages, cache: PagedCache) -> None:
+    """Moves the pages in use to the front of every layer's pool."""
+    _check(_native().pages_compact(C.addressof(pages.desc), C.addressof(cache.descs), len(cache.layers)), "lisa_pages_compact")
+
+
+def lisa_pages_copy(cache: PagedCache, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """Copies page src[i] to dst[i] in every layer (int32 on the device)."""
+    for x in (src, dst):
+        assert x.dtype == torch.int32 and x.is_cuda and x.is_contiguous() and x.shape == src.shape and x.dim() == 1
+    _check(load().lisa_pages_copy(cache.descs, len(cache.layers), src.data_ptr(), dst.data_ptr(), src.numel(), _stream()), "lisa_pages_copy")
 
 
 def lisa_check() -> int:

@@ -22,6 +22,13 @@ decltype(&lisa_kvcache_append) p_append;
 decltype(&lisa_kvcache_append_layer) p_append_layer;
 decltype(&lisa_project) p_project;
 decltype(&lisa_workspace_bytes) p_workspace_bytes;
+decltype(&lisa_paged_append) p_paged_append;
+decltype(&lisa_paged_read) p_paged_read;
+decltype(&lisa_attn_anchor_paged) p_anchor_paged;
+decltype(&lisa_attn_shared_decode_paged) p_shared_paged;
+decltype(&lisa_pages_fork) p_pages_fork;
+decltype(&lisa_pages_reserve) p_pages_reserve;
+decltype(&lisa_pages_compact) p_pages_compact;
 
 PyObject *s_qp, *s_kp, *s_w1, *s_w2, *s_b1, *s_b2, *s_act, *s_integrate, *s_ffn_layers;
 
@@ -306,10 +313,164 @@ PyObject* py_project(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- paged 8-bit cache: shapes are checked here, as the C structs carry no more than they need ----
+void require(bool ok, const char* msg) { if (!ok) fail(PyExc_AssertionError, msg); }
+const at::Tensor& on_device(PyObject* o) {
+    const at::Tensor& t = tensor(o);
+    require(t.is_cuda(), "expected a CUDA tensor");
+    return t;
+}
+// int32 [>= n], contiguous, or None
+const int32_t* counts_of(PyObject* o, int64_t n) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = on_device(o);
+    require(t.scalar_type() == at::kInt && t.dim() == 1 && t.size(0) >= n && t.is_contiguous(), "expected a contiguous int32 tensor with a value per sequence");
+    return t.data_ptr<int32_t>();
+}
+lisa_page_table table_of(PyObject* o, int64_t B) {
+    const at::Tensor& t = on_device(o);
+    require(t.scalar_type() == at::kInt && t.dim() == 2 && t.size(0) >= B && t.stride(1) == 1, "expected an int32 page table [B, max_pages] with contiguous rows");
+    return lisa_page_table{t.data_ptr<int32_t>(), t.stride(0), (int32_t)t.size(0), (int32_t)t.size(1)};
+}
+// A row of scores [>= B, >= Hq, >= L]
+void row_of(PyObject* o, int64_t B, int64_t Hq, int64_t L, void** p, int64_t* sb, int64_t* sh, int32_t* dt) {
+    const at::Tensor& t = on_device(o);
+    require(t.dim() == 3 && t.stride(2) == 1 && t.size(0) >= B && t.size(1) >= Hq && t.size(2) >= L, "expected score rows [B,Hq,L] with contiguous L");
+    *p = t.data_ptr(); *sb = t.stride(0); *sh = t.stride(1); *dt = dtype(t);
+}
+lisa_tensor head_rows(PyObject* o, int64_t B, int64_t n, int64_t H, int64_t x) {
+    const at::Tensor& t = on_device(o);
+    require(t.dim() == 4 && t.size(0) == B && t.size(1) == n && t.size(2) == H && t.size(3) == x, "a tensor's shape does not match the call's");
+    return tensor4(t);
+}
+
+// (layer descriptor's address, table, k or k', v, first, counts)
+template <typename F>
+PyObject* paged_rows(PyObject* const* a, Py_ssize_t n, F& entry) {
+    return call([&]() -> long {
+        expect(n, 6);
+        lisa_paged_rows_args p{};
+        p.struct_size = sizeof(p);
+        p.layer = address<const lisa_paged_layer*>(a[0]);
+        const at::Tensor& v = on_device(a[3]);
+        require(v.dim() == 4, "expected rows [B,n,Hkv,x]");
+        p.B = (int32_t)v.size(0); p.n = (int32_t)v.size(1);
+        p.table = table_of(a[1], p.B);
+        p.v = head_rows(a[3], p.B, p.n, p.layer->Hkv, p.layer->d);
+        p.k_or_kp = head_rows(a[2], p.B, p.n, p.layer->Hkv, p.layer->kind == LISA_CACHE_SHARED ? p.layer->r : p.layer->d);
+        p.first = counts_of(a[4], p.B); p.counts = counts_of(a[5], p.B);
+        lisa_stream_t s = stream();
+        return unlocked([&] { return entry(&p, s); });
+    });
+}
+PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return paged_rows(a, n, p_paged_append); }
+PyObject* py_paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) { return paged_rows(a, n, p_paged_read); }
+
+// (q, layer descriptor's address, table, L, seq_lens, out, out_scores, workspace)
+PyObject* py_anchor_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call([&]() -> long {
+        expect(n, 8);
+        const at::Tensor& q = on_device(a[0]);
+        lisa_paged_anchor_args p{};
+        p.struct_size = sizeof(p);
+        p.cache = address<const lisa_paged_layer*>(a[1]);
+        require(q.dim() == 4 && q.size(1) == 1, "expected q [B,1,Hq,d]");
+        p.B = (int32_t)q.size(0); p.Hq = (int32_t)q.size(2); p.L = (int32_t)integer(a[3]);
+        p.q = head_rows(a[0], p.B, 1, p.Hq, p.cache->d);
+        p.o = head_rows(a[5], p.B, 1, p.Hq, p.cache->d);
+        p.table = table_of(a[2], p.B);
+        p.seq_lens = counts_of(a[4], p.B);
+        if (a[6] != Py_None) row_of(a[6], p.B, p.Hq, p.L, &p.out_scores, &p.scores_stride_b, &p.scores_stride_h, &p.scores_dtype);
+        Scratch ws(a[7], LISA_OP_ANCHOR_PAGED, &p);
+        if (ws.status != LISA_OK) return ws.status;
+        p.workspace = ws.p; p.workspace_bytes = ws.bytes;
+        lisa_stream_t s = stream();
+        return unlocked([&] { return p_anchor_paged(&p, s); });
+    });
+}
+
+// (prev_scores, link, layer descriptor's address, table, L, seq_lens, out, out_scores, workspace)
+PyObject* py_shared_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call([&]() -> long {
+        expect(n, 9);
+        lisa_paged_shared_args p{};
+        p.struct_size = sizeof(p);
+        const at::Tensor& prev = on_device(a[0]);
+        p.cache = address<const lisa_paged_layer*>(a[2]);
+        p.L = (int32_t)integer(a[4]);
+        p.link = link(a[1]);
+        Ref qp(PyObject_GetAttr(a[1], s_qp));
+        const at::Tensor& q = on_device(qp.o);
+        require(prev.dim() == 3 && q.size(1) == 1, "expected score rows [B,Hq,L] and Q' [B,1,Hq,r]");
+        p.B = (int32_t)q.size(0); p.Hq = (int32_t)q.size(2);
+        const bool concat = p.link.integrate == LISA_INTEGRATE_CONCAT, two = p.link.ffn_layers == 2;
+        auto weight = [&](PyObject* name, int64_t rows, int64_t cols) {   // [rows, cols], or [cols] where rows is 0; None is the library's to judge
+            Ref w(PyObject_GetAttr(a[1], name));
+            if (w.o == Py_None) return;
+            const at::Tensor& t = on_device(w.o);
+            require(rows ? t.dim() == 2 && t.size(0) == rows && t.size(1) == cols : t.numel() == cols, "the aligner's weights do not match its heads and hidden width");
+        };
+        if (p.link.integrate != LISA_INTEGRATE_PLUS) {
+            weight(s_w1, concat ? 2 * p.Hq : p.Hq, p.link.m);
+            weight(s_b1, 0, p.link.m);
+            if (two) { weight(s_w2, p.link.m, p.Hq); weight(s_b2, 0, p.Hq); }
+        }
+        int32_t dt = 0;
+        void* row = nullptr;
+        row_of(a[0], p.B, p.Hq, p.L, &row, &p.prev_stride_b, &p.prev_stride_h, &p.scores_dtype);
+        p.prev_scores = row;
+        p.o = head_rows(a[6], p.B, 1, p.Hq, p.cache->d);
+        p.table = table_of(a[3], p.B);
+        p.seq_lens = counts_of(a[5], p.B);
+        if (a[7] != Py_None) {
+            row_of(a[7], p.B, p.Hq, p.L, &p.out_scores, &p.scores_stride_b, &p.scores_stride_h, &dt);
+            require(dt == p.scores_dtype, "out_scores: prev_scores' type");
+        }
+        Scratch ws(a[8], LISA_OP_SHARED_DECODE_PAGED, &p);
+        if (ws.status != LISA_OK) return ws.status;
+        p.workspace = ws.p; p.workspace_bytes = ws.bytes;
+        lisa_stream_t s = stream();
+        return unlocked([&] { return p_shared_paged(&p, s); });
+    });
+}
+
+// (pages descriptor's address, parent)
+PyObject* py_pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call([&]() -> long {
+        expect(n, 2);
+        const lisa_pages* p = address<const lisa_pages*>(a[0]);
+        const int32_t* parent = counts_of(a[1], p->B);
+        lisa_stream_t s = stream();
+        return unlocked([&] { return p_pages_fork(p, parent, s); });
+    });
+}
+// (pages descriptor's address, layer descriptors' address, layers, n_new)
+PyObject* py_pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call([&]() -> long {
+        expect(n, 4);
+        const lisa_pages* p = address<const lisa_pages*>(a[0]);
+        const lisa_paged_layer* layers = address<const lisa_paged_layer*>(a[1]);
+        const int32_t n_layers = (int32_t)integer(a[2]), *n_new = counts_of(a[3], p->B);
+        lisa_stream_t s = stream();
+        return unlocked([&] { return p_pages_reserve(p, layers, n_layers, n_new, s); });
+    });
+}
+// (pages descriptor's address, layer descriptors' address, layers)
+PyObject* py_pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call([&]() -> long {
+        expect(n, 3);
+        const lisa_pages* p = address<const lisa_pages*>(a[0]);
+        const lisa_paged_layer* layers = address<const lisa_paged_layer*>(a[1]);
+        const int32_t n_layers = (int32_t)integer(a[2]);
+        lisa_stream_t s = stream();
+        return unlocked([&] { return p_pages_compact(p, layers, n_layers, s); });
+    });
+}
+
 // The addresses of the library's entry points, in this order.
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call([&]() -> long {
-        expect(n, 8);
+        expect(n, 15);
         p_anchor = reinterpret_cast<decltype(p_anchor)>(address<void*>(a[0]));
         p_prefill = reinterpret_cast<decltype(p_prefill)>(address<void*>(a[1]));
         p_carry = reinterpret_cast<decltype(p_carry)>(address<void*>(a[2]));
@@ -318,13 +479,22 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
         p_append_layer = reinterpret_cast<decltype(p_append_layer)>(address<void*>(a[5]));
         p_project = reinterpret_cast<decltype(p_project)>(address<void*>(a[6]));
         p_workspace_bytes = reinterpret_cast<decltype(p_workspace_bytes)>(address<void*>(a[7]));
+        p_paged_append = reinterpret_cast<decltype(p_paged_append)>(address<void*>(a[8]));
+        p_paged_read = reinterpret_cast<decltype(p_paged_read)>(address<void*>(a[9]));
+        p_anchor_paged = reinterpret_cast<decltype(p_anchor_paged)>(address<void*>(a[10]));
+        p_shared_paged = reinterpret_cast<decltype(p_shared_paged)>(address<void*>(a[11]));
+        p_pages_fork = reinterpret_cast<decltype(p_pages_fork)>(address<void*>(a[12]));
+        p_pages_reserve = reinterpret_cast<decltype(p_pages_reserve)>(address<void*>(a[13]));
+        p_pages_compact = reinterpret_cast<decltype(p_pages_compact)>(address<void*>(a[14]));
         return 0;
     });
 }
 
 #define LISA_METHOD(name_) {#name_, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name_)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LISA_METHOD(anchor), LISA_METHOD(prefill), LISA_METHOD(carry), LISA_METHOD(decode), LISA_METHOD(append),
-                         LISA_METHOD(append_layer), LISA_METHOD(project), LISA_METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                         LISA_METHOD(append_layer), LISA_METHOD(project), LISA_METHOD(paged_append), LISA_METHOD(paged_read),
+                         LISA_METHOD(anchor_paged), LISA_METHOD(shared_paged), LISA_METHOD(pages_fork), LISA_METHOD(pages_reserve),
+                         LISA_METHOD(pages_compact), LISA_METHOD(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lisa_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -53,7 +53,8 @@ __device__ __forceinline__ float act_apply(float x, int act) {
     return x;
 }
 
-// Device status words (this device's copy): [0] cache appends dropped, [1] bounded waits that ran out.
+// Device status words (this device's copy): [0] cache appends dropped, page ids and parents out of range, [1] bounded waits that ran out,
+// [2] reserves that found too few pages.
 // Host function; returns the device address to hand to kernels, or nullptr if the lookup failed.
 int* status_words();
 

@@ -4,7 +4,8 @@
 #include <cstring>
 #include <mutex>
 
-#include "common.cuh"
+#include "api_checks.cuh"
+#include "paged_common.cuh"
 
 namespace lisa {
 
@@ -65,47 +66,13 @@ cudaError_t allow_smem(const void* kernel, size_t bytes, bool all_shared) {
     return cudaSuccess;
 }
 
-namespace {
-
 lisa_status_t cuda_fail(cudaError_t e) {
     t_last_cuda_error = (int)e;
     (void)cudaGetLastError();  // do not let a non-sticky error leak into the next call's launch check
     return LISA_ERR_CUDA;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool dtype_ok(int dt) { return dt == LISA_F32 || dt == LISA_BF16; }
-size_t esize(int dt) { return dt == LISA_BF16 ? 2 : 4; }
-
-lisa_status_t check_tensor(const lisa_tensor& t) {
-    if (!t.ptr || !dtype_ok(t.dtype) || !aligned16(t.ptr)) return LISA_ERR_INVALID_ARG;
-    return LISA_OK;
-}
-
-lisa_status_t check_dims(int B, int N, int Hq, int Hkv, int d) {
-    if (B < 1 || N < 1 || Hq < 1 || Hkv < 1 || d < 1) return LISA_ERR_INVALID_ARG;
-    if (Hq % Hkv != 0) return LISA_ERR_INVALID_ARG;
-    if (Hq > kMaxHeads) return LISA_ERR_UNSUPPORTED;
-    if (d != 32 && d != 64 && d != 128) return LISA_ERR_UNSUPPORTED;
-    return LISA_OK;
-}
-
-lisa_status_t check_link(const lisa_link& l, int Hq, bool prefill) {
-    if (l.r < 1) return LISA_ERR_INVALID_ARG;
-    if (l.r > kMaxRank) return LISA_ERR_UNSUPPORTED;
-    if (l.integrate < LISA_INTEGRATE_ADD || l.integrate > LISA_INTEGRATE_PLUS) return LISA_ERR_INVALID_ARG;
-    lisa_status_t st = check_tensor(l.qp);
-    if (st != LISA_OK) return st;
-    if (prefill && (st = check_tensor(l.kp)) != LISA_OK) return st;
-    if (l.integrate == LISA_INTEGRATE_PLUS) return LISA_OK;
-    if (l.act < LISA_ACT_NONE || l.act > LISA_ACT_SILU) return LISA_ERR_INVALID_ARG;
-    if (l.ffn_layers != 1 && l.ffn_layers != 2) return LISA_ERR_INVALID_ARG;
-    if (!dtype_ok(l.w_dtype) || !l.w1 || l.m < 1) return LISA_ERR_INVALID_ARG;
-    if (l.m > kMaxHidden) return LISA_ERR_UNSUPPORTED;
-    if (l.ffn_layers == 2 && !l.w2) return LISA_ERR_INVALID_ARG;
-    if (l.ffn_layers == 1 && l.m != Hq) return LISA_ERR_INVALID_ARG;
-    return LISA_OK;
-}
+namespace {
 
 lisa_status_t check_cache(const lisa_kvcache_layer* c, int kind, bool need_ptrs) {
     if (!c || c->kind != kind || !dtype_ok(c->dtype)) return LISA_ERR_INVALID_ARG;
@@ -128,12 +95,6 @@ size_t max_optin_smem() {
         return 232448;
     }
     return (size_t)v;
-}
-
-lisa_status_t check_workspace(const void* ws, size_t have, size_t need) {
-    if (need == 0) return LISA_OK;
-    if (!ws || have < need || !aligned16(ws)) return LISA_ERR_WORKSPACE;
-    return LISA_OK;
 }
 
 lisa_status_t validate_prefill(const lisa_shared_prefill_args* a) {
@@ -203,6 +164,7 @@ const char* lisa_status_string(int status) {
         case LISA_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case LISA_ERR_CUDA: return "CUDA error";
         case LISA_ERR_TIMEOUT: return "device-side wait timed out";
+        case LISA_ERR_NO_PAGES: return "not enough free pages";
         default: return "unknown status";
     }
 }
@@ -311,6 +273,20 @@ lisa_status_t lisa_workspace_bytes(int32_t op, const void* args, size_t* bytes) 
         const lisa_shared_decode_args* a = static_cast<const lisa_shared_decode_args*>(args);
         if (a->struct_size != sizeof(lisa_shared_decode_args) || !a->cache) return LISA_ERR_INVALID_ARG;
         *bytes = decode_workspace(a->B, a->Hq, a->cache->d, a->L);
+        return LISA_OK;
+    }
+    if (op == LISA_OP_ANCHOR_PAGED) {
+        const lisa_paged_anchor_args* a = static_cast<const lisa_paged_anchor_args*>(args);
+        if (a->struct_size != sizeof(lisa_paged_anchor_args) || !a->cache || check_dims(a->B, 1, a->Hq, a->cache->Hkv, a->cache->d) != LISA_OK || a->L < 1)
+            return LISA_ERR_INVALID_ARG;
+        *bytes = paged_anchor_workspace(a->B, a->Hq, a->cache->Hkv, a->cache->d, a->L);
+        return LISA_OK;
+    }
+    if (op == LISA_OP_SHARED_DECODE_PAGED) {
+        const lisa_paged_shared_args* a = static_cast<const lisa_paged_shared_args*>(args);
+        if (a->struct_size != sizeof(lisa_paged_shared_args) || !a->cache || check_dims(a->B, 1, a->Hq, a->cache->Hkv, a->cache->d) != LISA_OK || a->L < 1)
+            return LISA_ERR_INVALID_ARG;
+        *bytes = paged_shared_workspace(a->B, a->Hq, a->cache->Hkv, a->cache->d, a->L);
         return LISA_OK;
     }
     return LISA_ERR_INVALID_ARG;
@@ -536,10 +512,11 @@ lisa_status_t lisa_check(lisa_stream_t stream) {
     if (!dev) return cuda_fail(cudaErrorUnknown);
     int host[4] = {0, 0, 0, 0};
     if ((e = cudaMemcpy(host, dev, sizeof(host), cudaMemcpyDeviceToHost)) != cudaSuccess) return cuda_fail(e);
-    if (host[0] || host[1]) {
+    if (host[0] || host[1] || host[2]) {
         if ((e = cudaMemset(dev, 0, sizeof(host))) != cudaSuccess) return cuda_fail(e);
     }
     if (host[1]) return LISA_ERR_TIMEOUT;
+    if (host[2]) return LISA_ERR_NO_PAGES;
     if (host[0]) return LISA_ERR_INVALID_ARG;
     return LISA_OK;
 }

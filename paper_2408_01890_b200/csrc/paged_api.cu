@@ -1,0 +1,184 @@
+// C-ABI entry points of the paged 8-bit cache: host-side validation and dispatch.
+#include "api_checks.cuh"
+#include "paged_common.cuh"
+
+namespace lisa {
+namespace {
+
+constexpr int kMaxPositions = 1 << 30;   // of a sequence: position arithmetic stays within 32 bits
+constexpr int kMaxGrid = 65535;          // sequences are a grid's second or third coordinate
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+lisa_status_t check_layer(const lisa_paged_layer* c, bool need_ptr) {
+    if (!c || (c->kind != LISA_CACHE_STANDARD && c->kind != LISA_CACHE_SHARED)) return LISA_ERR_INVALID_ARG;
+    if (c->dtype != LISA_S8 && c->dtype != LISA_E4M3) return LISA_ERR_INVALID_ARG;
+    if (c->Hkv < 1 || c->n_pages < 1) return LISA_ERR_INVALID_ARG;
+    if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return LISA_ERR_INVALID_ARG;
+    if (c->Hkv > kMaxHeads) return LISA_ERR_UNSUPPORTED;
+    if (c->d != 32 && c->d != 64 && c->d != 128) return LISA_ERR_UNSUPPORTED;
+    if (c->kind == LISA_CACHE_SHARED) {
+        if (c->r < 1) return LISA_ERR_INVALID_ARG;
+        if (c->r > kMaxRank) return LISA_ERR_UNSUPPORTED;
+    }
+    if (need_ptr && (!c->pages || !aligned(c->pages, 128))) return LISA_ERR_INVALID_ARG;
+    return LISA_OK;
+}
+
+lisa_status_t check_table(const lisa_page_table& t, const lisa_paged_layer& c, int B) {
+    if (!t.pages || !aligned(t.pages, 4) || t.B < B || t.max_pages < 1 || t.stride < 0) return LISA_ERR_INVALID_ARG;
+    if (t.B > 1 && t.stride < t.max_pages) return LISA_ERR_INVALID_ARG;
+    if (t.max_pages > kMaxPositions / c.page_tokens) return LISA_ERR_UNSUPPORTED;
+    return LISA_OK;
+}
+
+// B, L, heads, layer and table of a decode step
+lisa_status_t check_step(int B, int Hq, int L, const lisa_paged_layer* c, int kind, const lisa_page_table& t) {
+    lisa_status_t st = check_layer(c, true);
+    if (st != LISA_OK) return st;
+    if (c->kind != kind) return LISA_ERR_INVALID_ARG;
+    if ((st = check_dims(B, 1, Hq, c->Hkv, c->d)) != LISA_OK) return st;
+    if (B > kMaxGrid) return LISA_ERR_UNSUPPORTED;
+    if ((st = check_table(t, *c, B)) != LISA_OK) return st;
+    return L < 1 || L > t.max_pages * c->page_tokens ? LISA_ERR_INVALID_ARG : LISA_OK;
+}
+
+// A row of scores: fp32 or bf16, aligned to its type; NULL where that is allowed
+lisa_status_t check_row(const void* row, int dtype, bool needed) {
+    if (dtype != LISA_F32 && dtype != LISA_BF16) return LISA_ERR_INVALID_ARG;
+    if (!row) return needed ? LISA_ERR_INVALID_ARG : LISA_OK;
+    return aligned(row, dtype == LISA_BF16 ? 2 : 4) ? LISA_OK : LISA_ERR_INVALID_ARG;
+}
+
+lisa_status_t check_rows(const lisa_paged_rows_args* a) {
+    if (!a || a->struct_size != sizeof(lisa_paged_rows_args) || a->B < 1 || a->n < 1) return LISA_ERR_INVALID_ARG;
+    lisa_status_t st = check_layer(a->layer, true);
+    if (st != LISA_OK) return st;
+    const lisa_paged_layer& c = *a->layer;
+    if ((st = check_table(a->table, c, a->B)) != LISA_OK) return st;
+    if ((st = check_tensor(a->v)) != LISA_OK) return st;
+    // K' moves a value at a time: a slice of a wider row will do
+    if (c.kind == LISA_CACHE_STANDARD ? check_tensor(a->k_or_kp) != LISA_OK : !a->k_or_kp.ptr || !aligned(a->k_or_kp.ptr, esize(a->v.dtype))) return LISA_ERR_INVALID_ARG;
+    if (a->k_or_kp.dtype != a->v.dtype) return LISA_ERR_INVALID_ARG;
+    const int64_t vec = 16 / (int64_t)esize(a->v.dtype);
+    auto rows_ok = [&](const lisa_tensor& t) { return t.stride_b % vec == 0 && t.stride_n % vec == 0 && t.stride_h % vec == 0; };
+    if (!rows_ok(a->v) || (c.kind == LISA_CACHE_STANDARD && !rows_ok(a->k_or_kp))) return LISA_ERR_INVALID_ARG;
+    if (!aligned(a->first, 4) || !aligned(a->counts, 4)) return LISA_ERR_INVALID_ARG;
+    if (a->n > kMaxPositions || (int64_t)a->B * ((a->n + 2 * LISA_PAGE_BLOCK - 2) / LISA_PAGE_BLOCK) * c.Hkv > INT32_MAX) return LISA_ERR_UNSUPPORTED;
+    return LISA_OK;
+}
+
+lisa_status_t check_pages(const lisa_pages* p, bool with_work) {
+    if (!p || p->struct_size != sizeof(lisa_pages)) return LISA_ERR_INVALID_ARG;
+    if (p->B < 1 || p->max_pages < 1 || p->n_pages < 1) return LISA_ERR_INVALID_ARG;
+    if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128) return LISA_ERR_INVALID_ARG;
+    if (p->B > LISA_MAX_PAGE_ROWS || p->max_pages > kMaxPositions / p->page_tokens) return LISA_ERR_UNSUPPORTED;
+    if (p->table_stride < 0 || (p->B > 1 && p->table_stride < p->max_pages)) return LISA_ERR_INVALID_ARG;
+    if (!p->table || !p->lens || !p->refs || !aligned(p->table, 4) || !aligned(p->lens, 4) || !aligned(p->refs, 4)) return LISA_ERR_INVALID_ARG;
+    return with_work ? check_workspace(p->work, p->work_bytes, pages_work_bytes(p->B, p->n_pages)) : LISA_OK;
+}
+
+lisa_status_t check_layers(const lisa_paged_layer* layers, int n_layers) {
+    if (!layers || n_layers < 1 || n_layers > LISA_MAX_LAYERS) return LISA_ERR_INVALID_ARG;
+    for (int l = 0; l < n_layers; ++l) {
+        const lisa_status_t st = check_layer(layers + l, true);
+        if (st != LISA_OK) return st;
+        if (layers[l].page_tokens != layers[0].page_tokens) return LISA_ERR_INVALID_ARG;
+    }
+    return LISA_OK;
+}
+
+// Every layer's pool has every page that the bookkeeping knows
+lisa_status_t check_pools(const lisa_pages* p, const lisa_paged_layer* layers, int n_layers) {
+    const lisa_status_t st = check_layers(layers, n_layers);
+    if (st != LISA_OK) return st;
+    for (int l = 0; l < n_layers; ++l)
+        if (layers[l].n_pages < p->n_pages || layers[l].page_tokens != p->page_tokens) return LISA_ERR_INVALID_ARG;
+    return LISA_OK;
+}
+
+lisa_status_t done(cudaError_t e) { return e == cudaSuccess ? LISA_OK : cuda_fail(e); }
+
+}  // namespace
+}  // namespace lisa
+
+using namespace lisa;
+
+extern "C" {
+
+lisa_status_t lisa_paged_layout_of(const lisa_paged_layer* layer, lisa_paged_layout* layout) {
+    const lisa_status_t st = check_layer(layer, false);
+    if (st != LISA_OK) return st;
+    if (!layout) return LISA_ERR_INVALID_ARG;
+    *layout = paged_layout(*layer);
+    return LISA_OK;
+}
+
+lisa_status_t lisa_paged_append(const lisa_paged_rows_args* a, lisa_stream_t stream) {
+    const lisa_status_t st = check_rows(a);
+    return st != LISA_OK ? st : done(launch_paged_append(*a, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_paged_read(const lisa_paged_rows_args* a, lisa_stream_t stream) {
+    const lisa_status_t st = check_rows(a);
+    return st != LISA_OK ? st : done(launch_paged_read(*a, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_attn_anchor_paged(const lisa_paged_anchor_args* a, lisa_stream_t stream) {
+    if (!a || a->struct_size != sizeof(lisa_paged_anchor_args)) return LISA_ERR_INVALID_ARG;
+    lisa_status_t st = check_step(a->B, a->Hq, a->L, a->cache, LISA_CACHE_STANDARD, a->table);
+    if (st != LISA_OK) return st;
+    if ((st = check_tensor(a->q)) != LISA_OK || (st = check_tensor(a->o)) != LISA_OK) return st;
+    if (!aligned(a->seq_lens, 4) || (st = check_row(a->out_scores, a->scores_dtype, false)) != LISA_OK) return LISA_ERR_INVALID_ARG;
+    const size_t need = paged_anchor_workspace(a->B, a->Hq, a->cache->Hkv, a->cache->d, a->L);
+    if ((st = check_workspace(a->workspace, a->workspace_bytes, need)) != LISA_OK) return st;
+    return done(launch_paged_anchor(*a, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_attn_shared_decode_paged(const lisa_paged_shared_args* a, lisa_stream_t stream) {
+    if (!a || a->struct_size != sizeof(lisa_paged_shared_args)) return LISA_ERR_INVALID_ARG;
+    lisa_status_t st = check_step(a->B, a->Hq, a->L, a->cache, LISA_CACHE_SHARED, a->table);
+    if (st != LISA_OK) return st;
+    if (a->link.r != a->cache->r) return LISA_ERR_INVALID_ARG;
+    if ((st = check_link(a->link, a->Hq, false)) != LISA_OK || (st = check_tensor(a->o)) != LISA_OK) return st;
+    if (check_row(a->prev_scores, a->scores_dtype, true) != LISA_OK || check_row(a->out_scores, a->scores_dtype, false) != LISA_OK) return LISA_ERR_INVALID_ARG;
+    if (!aligned(a->seq_lens, 4) || (a->out_scores && a->out_scores == a->prev_scores)) return LISA_ERR_INVALID_ARG;
+    const size_t need = paged_shared_workspace(a->B, a->Hq, a->cache->Hkv, a->cache->d, a->L);
+    if ((st = check_workspace(a->workspace, a->workspace_bytes, need)) != LISA_OK) return st;
+    return done(launch_paged_shared(*a, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_pages_work_bytes(const lisa_pages* p, size_t* bytes) {
+    if (!p || !bytes || p->struct_size != sizeof(lisa_pages) || p->B < 1 || p->n_pages < 1) return LISA_ERR_INVALID_ARG;
+    *bytes = pages_work_bytes(p->B, p->n_pages);
+    return LISA_OK;
+}
+
+lisa_status_t lisa_pages_fork(const lisa_pages* p, const int32_t* parent, lisa_stream_t stream) {
+    const lisa_status_t st = check_pages(p, false);
+    if (st != LISA_OK) return st;
+    if (!parent || !aligned(parent, 4)) return LISA_ERR_INVALID_ARG;
+    return done(launch_pages_fork(*p, parent, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_pages_reserve(const lisa_pages* p, const lisa_paged_layer* layers, int32_t n_layers, const int32_t* n_new, lisa_stream_t stream) {
+    lisa_status_t st = check_pages(p, true);
+    if (st != LISA_OK || (st = check_pools(p, layers, n_layers)) != LISA_OK) return st;
+    if (!aligned(n_new, 4)) return LISA_ERR_INVALID_ARG;
+    return done(launch_pages_reserve(*p, layers, n_layers, n_new, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_pages_compact(const lisa_pages* p, const lisa_paged_layer* layers, int32_t n_layers, lisa_stream_t stream) {
+    lisa_status_t st = check_pages(p, true);
+    if (st != LISA_OK || (st = check_pools(p, layers, n_layers)) != LISA_OK) return st;
+    return done(launch_pages_compact(*p, layers, n_layers, static_cast<cudaStream_t>(stream)));
+}
+
+lisa_status_t lisa_pages_copy(const lisa_paged_layer* layers, int32_t n_layers, const int32_t* src, const int32_t* dst, int32_t n, lisa_stream_t stream) {
+    const lisa_status_t st = check_layers(layers, n_layers);
+    if (st != LISA_OK) return st;
+    if (n < 1 || !src || !dst || !aligned(src, 4) || !aligned(dst, 4)) return LISA_ERR_INVALID_ARG;
+    return done(launch_pages_copy(layers, n_layers, src, dst, n, static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"

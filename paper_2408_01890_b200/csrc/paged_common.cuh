@@ -1,0 +1,124 @@
+// What the kernels of the paged 8-bit cache share: the pool's device view, and codes as fp16 operands.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace lisa {
+
+constexpr int kPageBlock = LISA_PAGE_BLOCK;
+
+// A layer's pool and the sequences' page tables.  Offsets inside a page fit 32 bits (64 heads x 128 positions x 2 x 128 bytes: 2 MB);
+// page_bytes * id does not.
+struct PagedView {
+    uint8_t* pages;
+    int64_t page_bytes, table_stride;
+    const int32_t* table;
+    int32_t n_pages, max_pages, shift;   // positions of a page: 1 << shift
+    int32_t Hkv, d, r;
+    uint32_t v_off, s_off;
+    int* status;
+
+    __device__ __forceinline__ int page_tokens() const { return 1 << shift; }
+    // Sequence b's page of position pos (< max_pages << shift), or -1, counted, where the table names none.
+    __device__ __forceinline__ int page_of(int b, int pos, bool count) const {
+        const int id = table[b * table_stride + (pos >> shift)];
+        if ((uint32_t)id < (uint32_t)n_pages) return id;
+        if (count) atomicAdd(status, 1);
+        return -1;
+    }
+    __device__ __forceinline__ uint8_t* page(int id) const { return pages + (int64_t)id * page_bytes; }
+    // Byte offset of a row (position, or block of K') inside a page
+    __device__ __forceinline__ uint32_t row(int h, int pos) const { return ((uint32_t)(h << shift) + (pos & ((1 << shift) - 1))) * d; }
+    __device__ __forceinline__ uint32_t kp_block(int h, int pos) const {
+        return ((uint32_t)(h << (shift - 4)) + ((pos & ((1 << shift) - 1)) >> 4)) * (r * kPageBlock);
+    }
+    // A block's pair of scales (K's, V's)
+    __device__ __forceinline__ float* scales(uint8_t* page, int h, int pos) const {
+        return reinterpret_cast<float*>(page + s_off) + 2 * ((h << (shift - 4)) + ((pos & ((1 << shift) - 1)) >> 4));
+    }
+};
+
+// Offsets of the layout that lisa.h states
+inline lisa_paged_layout paged_layout(const lisa_paged_layer& c) {
+    auto up = [](size_t n) { return (n + 127) & ~(size_t)127; };
+    const size_t rows = (size_t)c.Hkv * c.page_tokens, kw = c.kind == LISA_CACHE_SHARED ? c.r : c.d;
+    lisa_paged_layout l;
+    l.v_offset = up(rows * kw);
+    l.scale_offset = l.v_offset + rows * c.d;
+    l.page_bytes = up(l.scale_offset + rows / kPageBlock * 2 * sizeof(float));
+    return l;
+}
+
+inline PagedView paged_view(const lisa_paged_layer& c, const lisa_page_table& t) {
+    const lisa_paged_layout l = paged_layout(c);
+    PagedView v{};
+    v.pages = static_cast<uint8_t*>(c.pages);
+    v.page_bytes = (int64_t)l.page_bytes; v.table_stride = t.stride;
+    v.table = t.pages;
+    v.n_pages = c.n_pages; v.max_pages = t.max_pages;
+    for (v.shift = 4; (1 << v.shift) < c.page_tokens;) ++v.shift;
+    v.Hkv = c.Hkv; v.d = c.d; v.r = c.r;
+    v.v_off = (uint32_t)l.v_offset; v.s_off = (uint32_t)l.scale_offset;
+    v.status = status_words();
+    return v;
+}
+
+template <int FMT>
+__host__ __device__ constexpr float code_top() { return FMT == LISA_S8 ? 127.f : 448.f; }
+
+// y (in units of the scale) as a code: nearest even, saturating
+template <int FMT>
+__device__ __forceinline__ uint32_t to_code(float y) {
+    if constexpr (FMT == LISA_S8) {
+        return (uint32_t)__float2int_rn(fminf(fmaxf(y, -127.f), 127.f)) & 0xffu;
+    } else {
+        uint16_t v;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(0.f), "f"(y));
+        return v & 0xffu;
+    }
+}
+
+// The four codes of a word as two pairs of fp16, exactly (s8: 0x6400 | u is 1024 + u, so codes biased by 128 come out as 1152 + code)
+template <int FMT>
+__device__ __forceinline__ uint32_t pair16(uint32_t biased, bool high) {
+    uint32_t x;
+    if constexpr (FMT == LISA_S8) {
+        x = __byte_perm(biased, 0x64646464u, high ? 0x4342 : 0x4140);
+        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(x) : "h"((uint16_t)(high ? biased >> 16 : biased)));
+        return x;
+    }
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t biased(uint32_t w) { return FMT == LISA_S8 ? w ^ 0x80808080u : w; }
+
+// A word's code `i` as fp32
+template <int FMT>
+__device__ __forceinline__ float code_value(uint32_t w, int i) {
+    const uint32_t c = (w >> (8 * i)) & 0xffu;
+    if constexpr (FMT == LISA_S8) {
+        return (float)(int8_t)c;
+    } else {
+        uint32_t x;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(x) : "h"((uint16_t)c));
+        return __half2float(__ushort_as_half((unsigned short)(x & 0xffffu)));
+    }
+}
+
+// Host-side launchers of the paged cache
+cudaError_t launch_paged_append(const lisa_paged_rows_args& a, cudaStream_t s);
+cudaError_t launch_paged_read(const lisa_paged_rows_args& a, cudaStream_t s);
+size_t paged_anchor_workspace(int B, int Hq, int Hkv, int d, int L);
+size_t paged_shared_workspace(int B, int Hq, int Hkv, int d, int L);
+cudaError_t launch_paged_anchor(const lisa_paged_anchor_args& a, cudaStream_t s);
+cudaError_t launch_paged_shared(const lisa_paged_shared_args& a, cudaStream_t s);
+size_t pages_work_bytes(int B, int n_pages);
+cudaError_t launch_pages_fork(const lisa_pages& p, const int32_t* parent, cudaStream_t s);
+cudaError_t launch_pages_reserve(const lisa_pages& p, const lisa_paged_layer* layers, int n_layers, const int32_t* n_new, cudaStream_t s);
+cudaError_t launch_pages_compact(const lisa_pages& p, const lisa_paged_layer* layers, int n_layers, cudaStream_t s);
+cudaError_t launch_pages_copy(const lisa_paged_layer* layers, int n_layers, const int32_t* src, const int32_t* dst, int n, cudaStream_t s);
+
+}  // namespace lisa

@@ -1,0 +1,346 @@
+// The bookkeeping of pages: forking and freeing, allocation with copies on write, compaction, and the copying itself.
+//
+// Tables and counts are small (some hundred KB), so these kernels are bound by latency: one CTA plans, in registers and shared memory, with
+// two scans over the counts, and one kernel spread over the card moves the pages, bound by HBM (2 bytes per byte of page).  Free pages are taken in
+// ascending order and everything that is counted is an integer, so results do not depend on the order of threads.
+#include <algorithm>
+
+#include "paged_common.cuh"
+
+namespace lisa {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWarps = kPlanThreads / 32;
+constexpr int kCopyThreads = 256;
+constexpr int kPiece = 16384;            // bytes that a CTA copies at a time: four 16-byte loads of a thread in flight
+constexpr int kForkCols = 32;
+
+struct PagesDev {
+    int32_t *table, *lens, *refs;
+    int64_t stride;
+    int B, max_pages, n_pages, shift;
+    int *status;
+    // work: [0] moves, [1] pages in use; then source and destination of every move, and where each page went
+    int32_t *head, *src, *dst, *to;
+};
+
+PagesDev view_of(const lisa_pages& p) {
+    PagesDev v{};
+    v.table = p.table; v.lens = p.lens; v.refs = p.refs;
+    v.stride = p.table_stride;
+    v.B = p.B; v.max_pages = p.max_pages; v.n_pages = p.n_pages;
+    for (v.shift = 4; (1 << v.shift) < p.page_tokens;) ++v.shift;
+    v.status = status_words();
+    const int most = std::max(p.B, p.n_pages);
+    v.head = static_cast<int32_t*>(p.work);
+    v.src = v.head + 4; v.dst = v.src + most; v.to = v.dst + most;
+    return v;
+}
+
+// ------------------------------------------------------------------ fork
+// A CTA owns some columns of the table: it has read all of their rows before it writes one, so rows may change places.
+__global__ void __launch_bounds__(256) pages_fork_kernel(const __grid_constant__ PagesDev p, const int32_t* __restrict__ parent) {
+    extern __shared__ int32_t tile[];    // [B][kForkCols]; in the last CTA the lengths
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    chain_release();
+    chain_wait();
+    if (blockIdx.x == gridDim.x - 1) {
+        for (int i = tid; i < p.B; i += 256) tile[i] = p.lens[i];
+        __syncthreads();
+        for (int i = tid; i < p.B; i += 256) {
+            const int from = parent[i];
+            const bool ok = (uint32_t)from < (uint32_t)p.B;
+            if (!ok && from != -1) atomicAdd(p.status, 1);
+            p.lens[i] = ok ? tile[from] : 0;
+        }
+        return;
+    }
+    const int c = blockIdx.x * kForkCols + lane;
+    const bool in = c < p.max_pages;
+    for (int i = warp; i < p.B; i += 8) tile[i * kForkCols + lane] = in ? p.table[i * p.stride + c] : -1;
+    __syncthreads();
+    if (!in) return;
+    for (int i = warp; i < p.B; i += 8) {
+        const int from = parent[i];
+        const int old = tile[i * kForkCols + lane], now = (uint32_t)from < (uint32_t)p.B ? tile[from * kForkCols + lane] : -1;
+        if (now == old) continue;
+        if ((uint32_t)old < (uint32_t)p.n_pages) atomicSub(p.refs + old, 1);
+        if ((uint32_t)now < (uint32_t)p.n_pages) atomicAdd(p.refs + now, 1);
+        p.table[i * p.stride + c] = now;
+    }
+}
+
+// ------------------------------------------------------------------ planning
+// Exclusive sum over the CTA; *total is the sum of all.  `part` holds kPlanWarps + 1 values.
+__device__ __forceinline__ int block_scan(int v, int* part, int* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int upto = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    __syncthreads();                     // `part` may still be read from the scan before
+    if (lane == 31) part[warp] = upto;
+    __syncthreads();
+    if (warp == 0) {
+        int s = part[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += x;
+        }
+        part[lane] = s;
+    }
+    __syncthreads();
+    *total = part[kPlanWarps - 1];
+    return upto - v + (warp ? part[warp - 1] : 0);
+}
+
+constexpr int kPer = 4;                  // pages of a thread per round of a scan
+
+__global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __grid_constant__ PagesDev p, const int32_t* __restrict__ n_new) {
+    __shared__ int s_last[kPlanThreads], s_at[kPlanThreads + 1], s_have[kPlanThreads], part[kPlanWarps + 1];
+    __shared__ uint8_t s_copy[kPlanThreads];
+    const int tid = threadIdx.x, P = 1 << p.shift;
+    chain_release();
+    chain_wait();
+    int have = 0, need = 0, last = -1, refs = 0;
+    bool bad = false;
+    if (tid < p.B) {
+        const int64_t len = max(0, p.lens[tid]);
+        const int more = n_new ? max(0, n_new[tid]) : 1;
+        const int64_t h = (len + P - 1) >> p.shift, w = (len + more + P - 1) >> p.shift;
+        bad = w > p.max_pages || h > p.max_pages;
+        if (!bad) {
+            have = (int)h;
+            need = (int)w;
+            if ((len & (P - 1)) && more > 0) last = p.table[tid * p.stride + have - 1];
+            if ((uint32_t)last >= (uint32_t)p.n_pages) {
+                if (last != -1) atomicAdd(p.status, 1);
+                last = -1;
+            } else {
+                refs = p.refs[last];
+            }
+        }
+    }
+    s_last[tid] = last;
+    const int any_bad = __syncthreads_or(bad);
+    // writers of the same page in front of this row; each that copies leaves one entry fewer
+    int before = 0;
+    if (refs > 1)
+        for (int j = 0; j < tid; ++j) before += s_last[j] == last;
+    const bool copy = last >= 0 && refs - before > 1;
+    const int wanted = copy + need - have;
+    int total, moves, unused;
+    const int at = block_scan(wanted, part, &total);
+    const int move = block_scan(copy, part, &moves);
+    s_at[tid] = at;
+    s_have[tid] = have;
+    s_copy[tid] = copy;
+    if (tid == 0) p.head[0] = 0;
+    __syncthreads();
+    if (total == 0 && !any_bad) return;
+    // are there enough?
+    int free_pages = 0;
+    for (int base = 0; base < p.n_pages && free_pages < total; base += kPlanThreads * kPer) {
+        int mine = 0;
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int q = base + u * kPlanThreads + tid;
+            mine += q < p.n_pages && p.refs[q] == 0;
+        }
+        block_scan(mine, part, &unused);
+        free_pages += unused;
+    }
+    if (any_bad || free_pages < total) {
+        if (tid == 0) atomicAdd(p.status + 2, 1);
+        return;
+    }
+    if (copy) p.src[move] = last;
+    if (tid == 0) p.head[0] = moves;
+    __syncthreads();                     // (no count changes before every thread has made its plan)
+    if (copy) atomicSub(p.refs + last, 1);
+    // the k-th free page goes to the k-th page wanted
+    int found = 0;
+    for (int base = 0; base < p.n_pages && found < total; base += kPlanThreads) {
+        const int q = base + tid;
+        const bool free_page = q < p.n_pages && p.refs[q] == 0;
+        int sum;
+        const int k = found + block_scan(free_page, part, &sum);
+        found += sum;
+        if (!free_page || k >= total) continue;
+        int lo = 0, hi = p.B - 1;        // the last row with s_at <= k: rows that want none share their s_at with the next
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (s_at[mid] <= k) lo = mid; else hi = mid - 1;
+        }
+        const int local = k - s_at[lo];
+        const int slot = s_have[lo] + local - s_copy[lo];   // (a copy's: have - 1)
+        p.table[lo * p.stride + slot] = q;
+        p.refs[q] = 1;
+    }
+    __syncthreads();
+    if (copy) p.dst[move] = p.table[tid * p.stride + have - 1];
+}
+
+__global__ void __launch_bounds__(kPlanThreads) pages_compact_kernel(const __grid_constant__ PagesDev p) {
+    __shared__ int part[kPlanWarps + 1];
+    const int tid = threadIdx.x;
+    chain_release();
+    chain_wait();
+    int used = 0, sum;
+    for (int q = tid; q < p.n_pages; q += kPlanThreads) used += p.refs[q] > 0;
+    block_scan(used, part, &sum);
+    const int in_use = sum;
+    int holes = 0, movers = 0;
+    for (int base = 0; base < p.n_pages; base += kPlanThreads) {
+        const int q = base + tid;
+        const bool is_used = q < p.n_pages && p.refs[q] > 0;
+        const bool hole = q < in_use && !is_used, mover = q >= in_use && is_used;
+        if (q < p.n_pages) p.to[q] = q;
+        int s1;
+        // a round of the scan holds holes or movers or, in the one round around in_use, both: two 16-bit counts in one sum
+        const int k = block_scan((int)hole | (int)mover << 16, part, &s1);
+        if (hole) p.dst[holes + (k & 0xffff)] = q;
+        if (mover) p.src[movers + (k >> 16)] = q;
+        holes += s1 & 0xffff;
+        movers += s1 >> 16;
+    }
+    if (tid == 0) { p.head[0] = holes; p.head[1] = in_use; }
+    __syncthreads();
+    for (int i = tid; i < holes; i += kPlanThreads) {
+        const int from = p.src[i], into = p.dst[i];
+        p.to[from] = into;
+        p.refs[into] = p.refs[from];
+        p.refs[from] = 0;
+    }
+}
+
+// ------------------------------------------------------------------ moving
+struct CopyParams {
+    const int32_t *n_dev, *src, *dst;    // n_dev: device count, or null: n
+    int n, n_layers, pieces, n_pages;    // pieces of the largest page
+    int* status;                         // where ids are the caller's: checked, and counted here
+    // compaction: the tables follow
+    int32_t* table;
+    const int32_t* to;
+    int64_t stride;
+    int B, max_pages;
+    struct { uint8_t* pages; int64_t bytes; } layer[LISA_MAX_LAYERS];
+};
+
+__global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ CopyParams p) {
+    const int tid = threadIdx.x;
+    chain_release();
+    chain_wait();
+    if (p.table) {
+        const int64_t entries = (int64_t)p.B * p.max_pages;
+        for (int64_t e = blockIdx.x * (int64_t)kCopyThreads + tid; e < entries; e += (int64_t)gridDim.x * kCopyThreads) {
+            int32_t* at = p.table + e / p.max_pages * p.stride + e % p.max_pages;
+            if ((uint32_t)*at < (uint32_t)p.n_pages) *at = p.to[*at];
+        }
+    }
+    const int n = p.n_dev ? *p.n_dev : p.n;
+    const int64_t items = (int64_t)n * p.n_layers * p.pieces;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int piece = (int)(item % p.pieces), l = (int)(item / p.pieces % p.n_layers), i = (int)(item / p.pieces / p.n_layers);
+        const int64_t bytes = p.layer[l].bytes, at = (int64_t)piece * kPiece;
+        if (at >= bytes) continue;
+        const int from = p.src[i], into = p.dst[i];
+        if (p.status && ((uint32_t)from >= (uint32_t)p.n_pages || (uint32_t)into >= (uint32_t)p.n_pages)) {
+            if (tid == 0 && piece == 0 && l == 0) atomicAdd(p.status, 1);
+            continue;
+        }
+        const uint4* s = reinterpret_cast<const uint4*>(p.layer[l].pages + from * bytes + at);
+        uint4* d = reinterpret_cast<uint4*>(p.layer[l].pages + into * bytes + at);
+        const int vecs = (int)min((int64_t)kPiece, bytes - at) / 16;
+        uint4 v[kPiece / 16 / kCopyThreads];
+#pragma unroll
+        for (int u = 0; u < kPiece / 16 / kCopyThreads; ++u)
+            if (tid + u * kCopyThreads < vecs) v[u] = s[tid + u * kCopyThreads];
+#pragma unroll
+        for (int u = 0; u < kPiece / 16 / kCopyThreads; ++u)
+            if (tid + u * kCopyThreads < vecs) d[tid + u * kCopyThreads] = v[u];
+    }
+}
+
+void set_layers(CopyParams& c, const lisa_paged_layer* layers, int n_layers) {
+    c.n_layers = n_layers;
+    int64_t most = 0;
+    for (int l = 0; l < n_layers; ++l) {
+        const int64_t bytes = (int64_t)paged_layout(layers[l]).page_bytes;
+        c.layer[l].pages = static_cast<uint8_t*>(layers[l].pages);
+        c.layer[l].bytes = bytes;
+        most = std::max(most, bytes);
+    }
+    c.pieces = (int)((most + kPiece - 1) / kPiece);
+}
+
+// `most`: moves that there may be
+cudaError_t launch_copy(const CopyParams& c, int64_t most, cudaStream_t s) {
+    const int64_t items = most * c.n_layers * c.pieces, entries = c.table ? ((int64_t)c.B * c.max_pages + kCopyThreads - 1) / kCopyThreads : 0;
+    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(std::max(items, entries), (int64_t)sm_count() * 8));
+    const cudaError_t e = launch_chained(pages_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, s, c);
+    count_launches(1);
+    return e;
+}
+
+CopyParams planned_copy(const PagesDev& v) {
+    CopyParams c{};
+    c.n_dev = v.head; c.src = v.src; c.dst = v.dst;
+    c.n_pages = v.n_pages;
+    return c;
+}
+
+}  // namespace
+
+size_t pages_work_bytes(int B, int n_pages) { return (4 + 2 * (size_t)std::max(B, n_pages) + n_pages) * sizeof(int32_t); }
+
+cudaError_t launch_pages_fork(const lisa_pages& pages, const int32_t* parent, cudaStream_t s) {
+    const PagesDev v = view_of(pages);
+    if (!v.status) return cudaErrorUnknown;
+    const size_t smem = sizeof(int32_t) * (size_t)v.B * kForkCols;
+    cudaError_t e = allow_smem(pages_fork_kernel, smem);
+    if (e != cudaSuccess) return e;
+    e = launch_chained(pages_fork_kernel, dim3((v.max_pages + kForkCols - 1) / kForkCols + 1), dim3(256), smem, s, v, parent);
+    count_launches(1);
+    return e;
+}
+
+cudaError_t launch_pages_reserve(const lisa_pages& pages, const lisa_paged_layer* layers, int n_layers, const int32_t* n_new, cudaStream_t s) {
+    const PagesDev v = view_of(pages);
+    if (!v.status) return cudaErrorUnknown;
+    cudaError_t e = launch_chained(pages_reserve_kernel, dim3(1), dim3(kPlanThreads), 0, s, v, n_new);
+    count_launches(1);
+    if (e != cudaSuccess) return e;
+    CopyParams c = planned_copy(v);
+    set_layers(c, layers, n_layers);
+    return launch_copy(c, v.B, s);
+}
+
+cudaError_t launch_pages_compact(const lisa_pages& pages, const lisa_paged_layer* layers, int n_layers, cudaStream_t s) {
+    const PagesDev v = view_of(pages);
+    if (!v.status) return cudaErrorUnknown;
+    cudaError_t e = launch_chained(pages_compact_kernel, dim3(1), dim3(kPlanThreads), 0, s, v);
+    count_launches(1);
+    if (e != cudaSuccess) return e;
+    CopyParams c = planned_copy(v);
+    set_layers(c, layers, n_layers);
+    c.table = v.table; c.to = v.to; c.stride = v.stride; c.B = v.B; c.max_pages = v.max_pages;
+    return launch_copy(c, v.n_pages, s);
+}
+
+cudaError_t launch_pages_copy(const lisa_paged_layer* layers, int n_layers, const int32_t* src, const int32_t* dst, int n, cudaStream_t s) {
+    CopyParams c{};
+    c.src = src; c.dst = dst; c.n = n;
+    c.n_pages = INT32_MAX;
+    for (int l = 0; l < n_layers; ++l) c.n_pages = std::min(c.n_pages, layers[l].n_pages);
+    c.status = status_words();
+    if (!c.status) return cudaErrorUnknown;
+    set_layers(c, layers, n_layers);
+    return launch_copy(c, n, s);
+}
+
+}  // namespace lisa
