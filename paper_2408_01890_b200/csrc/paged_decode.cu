@@ -1,9 +1,8 @@
 // Decode step over a paged 8-bit cache: a standard layer (Eq. 1-2, last row) and a shared one (Sec. 5.2, decoding stage).
 //
-// attend   o_h = softmax_j(a_hj) V_j with a_hj = q_h.K_j / sqrt(d), or, for a shared layer, scores that the kernels below have left in
-//          a row.  One pass with a running maximum and sum: a warp streams its tiles of 16 positions (a tile never leaves a page) and keeps
-//          everything in registers; warps, and where a sequence is split CTAs, are joined at the end.
-// scores   a = W2^T act(W1^T prev + b1) + b2 + q'.K'_j / sqrt(r) and its variants, 128 positions (or fewer) of all heads to a CTA.
+// o_h = softmax_j(a_hj) V_j with a_hj = q_h.K_j / sqrt(d), or, for a shared layer, scores that paged_scores.cu has left in a row.  One pass with a
+// running maximum and sum: a warp streams its tiles of 16 positions (a tile never leaves a page) and keeps everything in registers; warps,
+// and where a sequence is split CTAs, are joined at the end.
 //
 // Both products over codes run on mma.sync m16n8k16 with the codes as the A operand, as fp16, which holds them exactly; scales are applied to the
 // fp32 results.  The other operand is q or the probabilities, brought to [2^13, 2^15) by a power of two and split into two fp16 terms (22 bits)
@@ -15,8 +14,7 @@
 #include <algorithm>
 #include <climits>
 
-#include "decode_common.cuh"
-#include "paged_common.cuh"
+#include "paged_decode.cuh"
 
 namespace lisa {
 namespace {
@@ -35,42 +33,6 @@ struct AttendParams {
     int64_t g_sb, g_sh;
     float *ws_m, *ws_l, *ws_o;     // [B][splits][Hq]( [d])
 };
-
-__device__ __forceinline__ int length_of(const int32_t* seq_lens, int b, int L) { return seq_lens ? max(0, min(seq_lens[b], L)) : L; }
-
-// d += a (16x16, row) . b (16x8, col), fp16 in, fp32 accumulate
-__device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// The two fp16 terms of x, side by side (low half: the leading term)
-__device__ __forceinline__ uint32_t two_terms(float x) {
-    const __half hi = __float2half_rn(x);
-    const __half2 v = __halves2half2(hi, __float2half_rn(x - __half2float(hi)));
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// One of the two terms
-__device__ __forceinline__ float term_of(float x, bool second) {
-    const float hi = __half2float(__float2half_rn(x));
-    return second ? x - hi : hi;
-}
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
-// Exponent of a finite positive value, from kLeastExp up; kLeastExp for zero and for what is not finite (which then stays so)
-constexpr int kLeastExp = -100;
-__device__ __forceinline__ int exponent(float x) {
-    const int e = (__float_as_int(x) >> 23 & 0xff) - 127;
-    return e == 128 ? kLeastExp : max(e, kLeastExp);
-}
 
 // W consecutive words
 template <int W>
@@ -422,109 +384,6 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
     st_elem(const_cast<void*>(p.o.ptr), b * p.o.sb + h * p.o.sh + threadIdx.x, p.o.dtype, den == 0.f ? 0.f : acc / den);
 }
 
-// ---------------------------------------------------------------------------------------------
-// Scores of a shared layer
-// ---------------------------------------------------------------------------------------------
-struct ScoresParams {
-    PagedView pool;
-    TView qp;
-    const int32_t* seq_lens;
-    int B, Hq, G, L;
-    const void* prev;              // fp32, or bf16 when row_bf16
-    int64_t prev_sb, prev_sh;
-    const void *w1, *b1, *w2, *b2;
-    int m, act, integrate, ffn_layers, w_dtype;
-    float* scores;                 // where attention reads them
-    int64_t s_sb, s_sh;
-    void* out_scores;              // the row for the next layer, where that is another one
-    int64_t sc_sb, sc_sh;
-    int row_bf16;
-};
-
-__device__ __forceinline__ void put_score(const ScoresParams& p, int b, int h, int pos, float v) {
-    p.scores[b * p.s_sb + h * p.s_sh + pos] = v;
-    if (p.out_scores) {
-        const int64_t to = b * p.sc_sb + h * p.sc_sh + pos;
-        if (p.row_bf16) st_row<true>(p.out_scores, to, v);
-        else st_row<false>(p.out_scores, to, v);
-    }
-}
-
-// Any head count, width, Integrate and weight type: a thread per position, fp32 throughout, weights in shared memory.
-constexpr int kGeneralThreads = 128;
-template <int FMT>
-__global__ void __launch_bounds__(kGeneralThreads) paged_scores_general_kernel(const __grid_constant__ ScoresParams p) {
-    extern __shared__ __align__(16) float smem[];
-    const int b = blockIdx.y, tid = threadIdx.x, pos = blockIdx.x * kGeneralThreads + tid;
-    const int Hq = p.Hq, r = p.pool.r, m = p.integrate == LISA_INTEGRATE_PLUS ? 0 : p.m;
-    const int h_in = p.integrate == LISA_INTEGRATE_CONCAT ? 2 * Hq : Hq;
-    float* w1_s = smem;                     // [h_in][m]
-    float* w2_s = w1_s + h_in * m;          // [m][Hq]
-    float* b1_s = w2_s + m * Hq;            // [m]
-    float* b2_s = b1_s + m;                 // [Hq]
-    float* qp_s = b2_s + Hq;                // [Hq][r]
-    chain_release();
-    if (m) {
-        for (int e = tid; e < h_in * m; e += kGeneralThreads) w1_s[e] = ld_elem(p.w1, e, p.w_dtype);
-        for (int e = tid; e < m; e += kGeneralThreads) b1_s[e] = ldw(p.b1, e, p.w_dtype);
-        if (p.ffn_layers == 2) {
-            for (int e = tid; e < m * Hq; e += kGeneralThreads) w2_s[e] = ld_elem(p.w2, e, p.w_dtype);
-            for (int e = tid; e < Hq; e += kGeneralThreads) b2_s[e] = ldw(p.b2, e, p.w_dtype);
-        }
-    }
-    chain_wait();
-    const int L = length_of(p.seq_lens, b, p.L);
-    if (blockIdx.x * kGeneralThreads >= L) return;
-    for (int e = tid; e < Hq * r; e += kGeneralThreads) qp_s[e] = ld_elem(p.qp.ptr, b * p.qp.sb + e / r * p.qp.sh + e % r, p.qp.dtype);
-    __syncthreads();
-    if (pos >= L) return;
-    const int id = p.pool.page_of(b, pos, (pos & (kPageBlock - 1)) == 0);
-    uint8_t* page = p.pool.page(max(id, 0));
-    const float inv_sqrt_r = rsqrtf((float)r);
-    float a[kMaxHeads], dl[kMaxHeads], hid[kMaxHidden];
-    for (int h = 0; h < Hq; ++h) {
-        const int64_t at = b * p.prev_sb + h * p.prev_sh + pos;
-        a[h] = p.row_bf16 ? ld_row<true>(p.prev, at) : ld_row<false>(p.prev, at);
-        float s = 0.f;
-        if (id >= 0) {
-            const uint8_t* k = page + p.pool.kp_block(h / p.G, pos) + (pos & (kPageBlock - 1));
-            for (int x = 0; x < r; ++x) s = fmaf(qp_s[h * r + x], code_value<FMT>(k[x * kPageBlock], 0), s);
-            s *= p.pool.scales(page, h / p.G, pos)[0] * inv_sqrt_r;
-        }
-        dl[h] = s;
-    }
-    if (p.integrate == LISA_INTEGRATE_PLUS) {
-        for (int h = 0; h < Hq; ++h) a[h] += dl[h];
-    } else {
-        for (int u = 0; u < m; ++u) {
-            float s = b1_s[u];
-            for (int x = 0; x < Hq; ++x) s = fmaf(a[x], w1_s[x * m + u], s);
-            if (p.integrate == LISA_INTEGRATE_CONCAT)
-                for (int x = 0; x < Hq; ++x) s = fmaf(dl[x], w1_s[(Hq + x) * m + u], s);
-            hid[u] = s;
-        }
-        if (p.ffn_layers == 1) {
-            for (int h = 0; h < Hq; ++h) a[h] = hid[h];
-        } else {
-            for (int u = 0; u < m; ++u) hid[u] = act_apply(hid[u], p.act);
-            for (int h = 0; h < Hq; ++h) {
-                float s = b2_s[h];
-                for (int u = 0; u < m; ++u) s = fmaf(hid[u], w2_s[u * Hq + h], s);
-                a[h] = s;
-            }
-        }
-        if (p.integrate == LISA_INTEGRATE_ADD)
-            for (int h = 0; h < Hq; ++h) a[h] += dl[h];
-    }
-    if (id < 0) return;
-    for (int h = 0; h < Hq; ++h) put_score(p, b, h, pos, a[h]);
-}
-
-size_t general_smem(const ScoresParams& p) {
-    const int h_in = p.integrate == LISA_INTEGRATE_CONCAT ? 2 * p.Hq : p.Hq, m = p.integrate == LISA_INTEGRATE_PLUS ? 0 : p.m;
-    return sizeof(float) * ((size_t)h_in * m + (size_t)m * p.Hq + m + p.Hq + (size_t)p.Hq * p.pool.r);
-}
-
 // ------------------------------------------------------------------ launches
 constexpr int kMinTiles = kUnit * kAttendWarps;           // of a CTA: less would leave warps without work
 constexpr int kSlots = 4;                                 // CTAs an SM is given at least, as long as there are tiles
@@ -575,16 +434,6 @@ cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
     return e;
 }
 
-template <int FMT>
-cudaError_t launch_scores(const ScoresParams& p, cudaStream_t s) {
-    const size_t smem = general_smem(p);
-    cudaError_t e = allow_smem(paged_scores_general_kernel<FMT>, smem);
-    if (e != cudaSuccess) return e;
-    e = launch_chained(paged_scores_general_kernel<FMT>, dim3((p.L + kGeneralThreads - 1) / kGeneralThreads, p.B), dim3(kGeneralThreads), smem, s, p);
-    count_launches(1);
-    return e;
-}
-
 }  // namespace
 
 size_t paged_anchor_workspace(int B, int Hq, int Hkv, int d, int L) { return part_bytes(B, Hq, Hkv, d, L); }
@@ -626,7 +475,7 @@ cudaError_t launch_paged_shared(const lisa_paged_shared_args& a, cudaStream_t s)
         c.out_scores = a.out_scores; c.sc_sb = a.scores_stride_b; c.sc_sh = a.scores_stride_h;
     }
     const bool s8 = a.cache->dtype == LISA_S8;
-    const cudaError_t e = s8 ? launch_scores<LISA_S8>(c, s) : launch_scores<LISA_E4M3>(c, s);
+    const cudaError_t e = launch_paged_scores(c, a.cache->dtype, s);
     if (e != cudaSuccess) return e;
     AttendParams p{};
     p.pool = c.pool;

@@ -1,0 +1,63 @@
+// What the kernels of the paged decode step share: operands of products over codes, and the parameters of a shared layer's scores.
+#pragma once
+#include "decode_common.cuh"
+#include "paged_common.cuh"
+
+namespace lisa {
+
+__device__ __forceinline__ int length_of(const int32_t* seq_lens, int b, int L) { return seq_lens ? max(0, min(seq_lens[b], L)) : L; }
+
+// d += a (16x16, row) . b (16x8, col), fp16 in, fp32 accumulate
+__device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// The two fp16 terms of x, side by side (low half: the leading term)
+__device__ __forceinline__ uint32_t two_terms(float x) {
+    const __half hi = __float2half_rn(x);
+    const __half2 v = __halves2half2(hi, __float2half_rn(x - __half2float(hi)));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// One of the two terms
+__device__ __forceinline__ float term_of(float x, bool second) {
+    const float hi = __half2float(__float2half_rn(x));
+    return second ? x - hi : hi;
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+// Exponent of a finite positive value, from kLeastExp up; kLeastExp for zero and for what is not finite (which then stays so)
+constexpr int kLeastExp = -100;
+__device__ __forceinline__ int exponent(float x) {
+    const int e = (__float_as_int(x) >> 23 & 0xff) - 127;
+    return e == 128 ? kLeastExp : max(e, kLeastExp);
+}
+
+// A shared layer's scores over the cache (paged_scores.cu)
+struct ScoresParams {
+    PagedView pool;
+    TView qp;
+    const int32_t* seq_lens;
+    int B, Hq, G, L;
+    const void* prev;              // fp32, or bf16 when row_bf16
+    int64_t prev_sb, prev_sh;
+    const void *w1, *b1, *w2, *b2;
+    int m, act, integrate, ffn_layers, w_dtype;
+    float* scores;                 // where attention reads them
+    int64_t s_sb, s_sh;
+    void* out_scores;              // the row for the next layer, where that is another one
+    int64_t sc_sb, sc_sh;
+    int row_bf16;
+};
+
+cudaError_t launch_paged_scores(const ScoresParams& p, int dtype, cudaStream_t s);
+
+}  // namespace lisa
