@@ -92,6 +92,17 @@ __device__ __forceinline__ uint32_t pair16(uint32_t biased, bool high) {
         return x;
     }
 }
+// The codes in bytes 0 and 2 (or 1 and 3) of a word, likewise
+template <int FMT>
+__device__ __forceinline__ uint32_t across16(uint32_t biased, bool odd) {
+    if constexpr (FMT == LISA_S8) {
+        const uint32_t x = __byte_perm(biased, 0x64646464u, odd ? 0x4341 : 0x4240);
+        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        return pair16<FMT>(__byte_perm(biased, 0u, odd ? 0x4431 : 0x4420), false);
+    }
+}
 template <int FMT>
 __device__ __forceinline__ uint32_t biased(uint32_t w) { return FMT == LISA_S8 ? w ^ 0x80808080u : w; }
 

@@ -8,11 +8,12 @@
 // fp32 results.  The other operand is q or the probabilities, brought to [2^13, 2^15) by a power of two and split into two fp16 terms (22 bits)
 // that take two neighbouring columns of B, so that the eight columns are four query heads: with few heads to a KV head the columns
 // are there anyway.  The sum of the two columns is what an fp32 product would give, up to 2^-22 of the largest term.
-// The A operands come straight from global memory, without shared memory: the order of d in q.K, of d in the rows of the output, and of
-// positions in P.V is free, so every lane's share of a fragment is 16 consecutive bytes of a row.
+// The order of d in q.K, of d in the rows of the output, and of positions in P.V is free, so every lane's share of a fragment is 16 consecutive
+// bytes of a row.
 // Bound by HBM: a position and head are d bytes of K and d of V.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "paged_decode.cuh"
 
@@ -34,33 +35,67 @@ struct AttendParams {
     float *ws_m, *ws_l, *ws_o;     // [B][splits][Hq]( [d])
 };
 
-// W consecutive words
-template <int W>
-__device__ __forceinline__ void ld_words(uint32_t* w, const uint8_t* p) {
-    if constexpr (W == 4) {
-        const uint4 v = ld_stream16(p);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    } else if constexpr (W == 2) {
-        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    } else {
-        asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-    }
-}
-
 // ---------------------------------------------------------------------------------------------
 // Attention of up to 4 NT query heads of one KV head.  Lane = (g, t) = (lane / 4, lane % 4) throughout.
+//
+// A warp takes units of two tiles.  Their rows come by cp.async into a ring of its own in shared memory, STAGES - 1 units ahead, so that loads stay
+// in flight whatever the warp computes and cost no registers (with the rows of one unit ahead in registers 64 x 4096 of the 13B shape took
+// 504 us, and 307 us for V alone).  Warps never wait for one another before the end.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
 constexpr int kUnit = 2;                                  // tiles that a warp takes at a time: its maximum is reduced once a unit
-constexpr int kBatch = 32 / kUnit;                        // units whose pages and scales the lanes hold
+constexpr int kUnitRows = kUnit * kPageBlock;
+constexpr int kBatch = 32 / kUnit;                        // units whose pages the lanes hold
+
+// A stage: K rows (or the given scores [heads][32]), V rows, {K's scale, V's scale} of each tile, whether its page is there
+template <int D, int H, bool GIVEN>
+struct Stage {
+    static constexpr int kFirst = GIVEN ? H * kUnitRows * 4 : kUnitRows * D, kV = kFirst, kScales = kV + kUnitRows * D, kThere = kScales + kUnit * 8;
+    static constexpr int kBytes = kThere + 16;
+    static constexpr int kCount = GIVEN ? 3 : 2;
+    static constexpr int kRing = kBytes * kCount;
+    static constexpr int kMerge = kAttendWarps * H * (D + 2) * 4;
+    static constexpr int kTotal = kRing * kAttendWarps > kMerge ? kRing * kAttendWarps : kMerge;
+    static constexpr int kCtas = H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
+};
+
+// 16, 8 or 4 bytes from global to shared memory, zeros where !ok (nothing is read then)
+template <int N>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) {
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(ok ? N : 0), "n"(N) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Rows lie with their 16-byte chunks permuted, so that the eight lanes of a shared-memory access meet eight different ones.  A K access is four
+// chunks of two neighbouring rows; a V access (ldmatrix) one chunk of eight rows, of which 64- and 32-byte rows put two and four beside one another.
+template <int D>
+__device__ __forceinline__ int k_chunk(int row, int c) { return D == 128 ? c ^ ((row & 1) << 2) : c; }
+template <int D>
+__device__ __forceinline__ int v_chunk(int row, int c) { return c ^ (D == 128 ? row & 7 : D == 64 ? row >> 1 & 3 : row >> 2 & 1); }
+
+template <int W>
+__device__ __forceinline__ void lds_words(uint32_t* w, const uint8_t* p) {
+    if constexpr (W == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (W == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
 
 template <int FMT, int D, int NT, bool GIVEN>
-__global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __grid_constant__ AttendParams p) {
-    constexpr int KW = D / 16, VW = D / 32, MT = D / 16;  // words of a lane per K row and per V row; tiles of 16 output columns
-    constexpr int H = 4 * NT;
-    __shared__ float s_m[kAttendWarps][H], s_l[kAttendWarps][H];
-    __shared__ __align__(16) float s_o[kAttendWarps][H][D];
+__global__ void __launch_bounds__(kAttendThreads, Stage<D, 4 * NT, GIVEN>::kCtas) paged_attend_kernel(const __grid_constant__ AttendParams p) {
+    constexpr int KW = D / 16, MT = D / 16;               // words of a lane per K row; tiles of 16 output columns
+    constexpr int H = 4 * NT, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
+    using S = Stage<D, H, GIVEN>;
+    extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int b = blockIdx.z, split = blockIdx.x, kvh = blockIdx.y / p.passes, pass = blockIdx.y % p.passes;
     const int h0 = kvh * p.G + pass * p.heads, nh = min(p.heads, p.G - pass * p.heads);
@@ -75,6 +110,56 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
             for (int e = tid; e < nh * D; e += kAttendThreads) st_elem(out, b * p.o.sb + (h0 + e / D) * p.o.sh + e % D, p.o.dtype, 0.f);
         return;
     }
+
+    const int units = (end - first + kUnit - 1) / kUnit, mine = units > warp ? (units - warp + kAttendWarps - 1) / kAttendWarps : 0;
+    auto tile_of = [&](int k) { return first + (warp + kAttendWarps * (k / kUnit)) * kUnit + k % kUnit; };   // this warp's k-th tile
+    auto id_of = [&](int k) {
+        const int tile = tile_of(k);
+        return k < mine * kUnit && tile < end ? pool.page_of(b, tile * kPageBlock, blockIdx.y == 0) : -1;
+    };
+    // lane i: page of tile i of the batch of units that is being asked for; the next batch's are loaded a batch ahead
+    int ids = id_of(lane), ids_next = id_of(32 + lane);
+
+    uint8_t* ring = smem + warp * S::kRing;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const int c_row = lane / LPR, c_col = lane % LPR;     // what this lane copies
+    auto ask = [&](int i, int stage) {                    // unit i into its stage: rows past the end are zeros
+        if (i < mine) {
+            const int at = i % kBatch * kUnit;
+            if (at == 0 && i > 0) {
+                ids = ids_next;
+                ids_next = id_of(i * kUnit + 32 + lane);
+            }
+            const uint32_t to = ring_at + stage * S::kBytes;
+            const int pos = tile_of(i * kUnit) * kPageBlock;          // (a unit's tiles are neighbours)
+            int id[kUnit];
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) {
+                id[u] = __shfl_sync(0xffffffffu, ids, at + u);
+                const uint8_t* src = pool.page(max(id[u], 0)) + pool.row(kvh, pos + u * kPageBlock) + lane * 16;
+                const int left = id[u] >= 0 ? L - pos - u * kPageBlock - c_row : INT_MIN;   // this lane's first row is there if it is above 0
+#pragma unroll
+                for (int k = 0; k < kPageBlock / RPI; ++k) {
+                    const int row = u * kPageBlock + k * RPI + c_row;
+                    if (!GIVEN) cp_async<16>(to + row * D + k_chunk<D>(row, c_col) * 16, src + k * 512, k * RPI < left);
+                    cp_async<16>(to + S::kV + row * D + v_chunk<D>(row, c_col) * 16, src + pool.v_off + k * 512, k * RPI < left);
+                }
+            }
+            if constexpr (GIVEN) {
+                const bool ok = pos + lane < L;
+                const float* src = p.given + b * p.g_sb + h0 * p.g_sh + (ok ? pos + lane : 0);
+                for (int h = 0; h < nh; ++h) cp_async<4>(to + (h * kUnitRows + lane) * 4, src + h * p.g_sh, ok);
+            }
+            if (lane < kUnit) {
+                const int mine_id = lane ? id[kUnit - 1] : id[0];
+                cp_async<8>(to + S::kScales + lane * 8, pool.scales(pool.page(max(mine_id, 0)), kvh, pos + lane * kPageBlock), mine_id >= 0);
+                reinterpret_cast<int*>(ring + stage * S::kBytes + S::kThere)[lane] = mine_id >= 0;
+            }
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S::kCount - 1; ++i) ask(i, i);
 
     // q as B fragments: column g is head g / 2's leading (even g) or second term
     uint32_t qf[NT][KW][2];
@@ -96,7 +181,7 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
             amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
             amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
             const int ex = exponent(amax);
-            const float up = pow2(13 - max(ex, -100));
+            const float up = pow2(13 - ex);
 #pragma unroll
             for (int w = 0; w < KW; ++w)
 #pragma unroll
@@ -106,62 +191,7 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
         }
     }
 
-    const int units = (end - first + kUnit - 1) / kUnit, mine = units > warp ? (units - warp + kAttendWarps - 1) / kAttendWarps : 0;
-    auto tile_of = [&](int k) { return first + (warp + kAttendWarps * (k / kUnit)) * kUnit + k % kUnit; };   // this warp's k-th tile
-    auto id_of = [&](int k) {
-        const int tile = tile_of(k);
-        return k < mine * kUnit && tile < end ? pool.page_of(b, tile * kPageBlock, blockIdx.y == 0) : -1;
-    };
-    // lane i: page and scales of tile i of the batch; the next batch's pages are asked for a batch ahead
-    int ids = id_of(lane), ids_next = id_of(32 + lane);
-    float ks = 0.f, vs = 0.f;
-    auto load_scales = [&](int k) {
-        ks = vs = 0.f;
-        if (ids >= 0) {
-            const float2 v = *reinterpret_cast<const float2*>(pool.scales(pool.page(ids), kvh, tile_of(k) * kPageBlock));
-            ks = v.x; vs = v.y;
-        }
-    };
-    load_scales(lane);
-
-    uint32_t kw[kUnit][2][KW], vw[kUnit][4][VW];
-    int id[kUnit];                                        // pages of the unit whose rows are being loaded
-    const uint32_t k_col = D == 128 ? 16 * t : 4 * KW * t, v_col = 4 * VW * g;
-    auto load_k = [&](int i) {                            // K rows g and g + 8 of the unit's tiles, zeros past the end
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u) {
-            const int pos = tile_of(i * kUnit + u) * kPageBlock + g;
-            const uint8_t* at = pool.page(max(id[u], 0)) + pool.row(kvh, pos) + k_col;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const bool ok = id[u] >= 0 && pos + 8 * e < L;
-#pragma unroll
-                for (int w = 0; w < KW; ++w) kw[u][e][w] = 0u;
-                if (ok) {
-                    constexpr int W = KW < 4 ? KW : 4;
-#pragma unroll
-                    for (int c = 0; c < KW / W; ++c) ld_words<W>(&kw[u][e][c * W], at + e * 8 * D + c * 64);
-                }
-            }
-        }
-    };
-    auto load_v = [&](int i, const int* page_ids) {       // V rows 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u) {
-            const int pos = tile_of(i * kUnit + u) * kPageBlock + 2 * t;
-            const uint8_t* at = pool.page(max(page_ids[u], 0)) + pool.v_off + pool.row(kvh, pos) + v_col;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int step = (e & 1) + (e >> 1) * 8;
-                const bool ok = page_ids[u] >= 0 && pos + step < L;
-#pragma unroll
-                for (int w = 0; w < VW; ++w) vw[u][e][w] = 0u;
-                if (ok) ld_words<VW>(vw[u][e], at + step * D);
-            }
-        }
-    };
-
-    float m[NT], l[NT], o[NT][MT][4], given[kUnit][NT][2];
+    float m[NT], l[NT], o[NT][MT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt] = -INFINITY;
@@ -173,75 +203,54 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
     }
     int r_exp = kLeastExp;                                // V enters as code * 2^13 scale / 2^r_exp
 
-    auto load_given = [&](int i) {
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int pos = tile_of(i * kUnit + u) * kPageBlock + g + 8 * e;
-                    given[u][nt][e] = pos < L && nt * 4 + t < nh ? p.given[b * p.g_sb + (h0 + nt * 4 + t) * p.g_sh + pos] : 0.f;
-                }
-    };
-
-    if (mine > 0) {
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u) id[u] = __shfl_sync(0xffffffffu, ids, u);
-        if constexpr (GIVEN) load_given(0);
-        else load_k(0);
-        load_v(0, id);
-    }
-    for (int i = 0; i < mine; ++i) {
-        const int at = i % kBatch * kUnit;
-        float ks_u[kUnit], vs_u[kUnit], s[kUnit][NT][2];
-        bool page_ok[kUnit];
+    for (int i = 0, stage = 0; i < mine; ++i, stage = stage + 1 == S::kCount ? 0 : stage + 1) {
+        cp_wait<S::kCount - 2>();
+        __syncwarp();                                     // unit i is there, and every lane has done with unit i - 1
+        ask(i + S::kCount - 1, stage == 0 ? S::kCount - 1 : stage - 1);
+        const uint8_t* st = ring + stage * S::kBytes;
+        const int pos0 = tile_of(i * kUnit) * kPageBlock + g;
+        float s[kUnit][NT][2], vs[kUnit];
+        bool there[kUnit];
 #pragma unroll
         for (int u = 0; u < kUnit; ++u) {
-            ks_u[u] = __shfl_sync(0xffffffffu, ks, at + u);
-            vs_u[u] = __shfl_sync(0xffffffffu, vs, at + u);
-            page_ok[u] = id[u] >= 0;
-        }
-        // scores
-        if constexpr (!GIVEN) {
-#pragma unroll
-            for (int u = 0; u < kUnit; ++u) {
+            const float2 sc = reinterpret_cast<const float2*>(st + S::kScales)[u];
+            vs[u] = sc.y;
+            there[u] = reinterpret_cast<const int*>(st + S::kThere)[u];
+            if constexpr (!GIVEN) {
                 float c[NT][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
+                uint32_t kw[2][KW];
+                constexpr int W = KW < 4 ? KW : 4;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row = u * kPageBlock + g + 8 * e;
+#pragma unroll
+                    for (int x = 0; x < KW / W; ++x)
+                        lds_words<W>(&kw[e][x * W], st + row * D + (D == 128 ? k_chunk<D>(row, 4 * x + t) * 16 : 4 * KW * t));
+                }
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
-                    const uint32_t x0 = biased<FMT>(kw[u][0][w]), x1 = biased<FMT>(kw[u][1][w]);
+                    const uint32_t x0 = biased<FMT>(kw[0][w]), x1 = biased<FMT>(kw[1][w]);
                     const uint32_t a0 = pair16<FMT>(x0, false), a1 = pair16<FMT>(x1, false), a2 = pair16<FMT>(x0, true), a3 = pair16<FMT>(x1, true);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma_f16(c[nt], a0, a1, a2, a3, qf[nt][w][0], qf[nt][w][1]);
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const float f = ks_u[u] * q_scale[nt];
+                    const float f = sc.x * q_scale[nt];
                     s[u][nt][0] = (c[nt][0] + c[nt][1]) * f;
                     s[u][nt][1] = (c[nt][2] + c[nt][3]) * f;
                 }
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int h = nt * 4 + t;
+                        s[u][nt][e] = h < nh ? reinterpret_cast<const float*>(st)[h * kUnitRows + u * kPageBlock + g + 8 * e] : 0.f;
+                    }
             }
-        } else {
-#pragma unroll
-            for (int u = 0; u < kUnit; ++u)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) { s[u][nt][0] = given[u][nt][0]; s[u][nt][1] = given[u][nt][1]; }
-        }
-        // the next unit's K (or scores) are asked for as soon as the registers are free
-        const bool more = i + 1 < mine;
-        if (more) {
-            if (i % kBatch == kBatch - 1) {
-                ids = ids_next;
-                load_scales((i + 1) * kUnit + lane);
-                ids_next = id_of((i + 1) * kUnit + 32 + lane);
-            }
-            const int next = (i + 1) % kBatch * kUnit;
-#pragma unroll
-            for (int u = 0; u < kUnit; ++u) id[u] = __shfl_sync(0xffffffffu, ids, next + u);
-            if constexpr (GIVEN) load_given(i + 1);
-            else load_k(i + 1);
         }
         // running maximum
 #pragma unroll
@@ -251,8 +260,8 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
             for (int u = 0; u < kUnit; ++u)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int pos = tile_of(i * kUnit + u) * kPageBlock + g + 8 * e;
-                    const bool on = page_ok[u] && pos < L;
+                    const int pos = pos0 + u * kPageBlock + 8 * e;
+                    const bool on = there[u] && pos < L;
                     if (!GIVEN && p.out_scores && on && nt * 4 + t < nh) {
                         const int64_t to = b * p.sc_sb + (h0 + nt * 4 + t) * p.sc_sh + pos;
                         if (p.row_bf16) st_row<true>(p.out_scores, to, s[u][nt][e]);
@@ -276,7 +285,7 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
         // V's scales enter with the probabilities; their common power of two follows the largest so far
         int ex = r_exp;
 #pragma unroll
-        for (int u = 0; u < kUnit; ++u) ex = max(ex, exponent(vs_u[u]));
+        for (int u = 0; u < kUnit; ++u) ex = max(ex, exponent(vs[u]));
         if (ex > r_exp) {
             const float f = pow2(max(r_exp - ex, -126));
 #pragma unroll
@@ -291,7 +300,7 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
 #pragma unroll
         for (int u = 0; u < kUnit; ++u) {
             uint32_t bf[NT][2];
-            const float f = vs_u[u] * up;
+            const float f = vs[u] * up;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float ref = m[nt] == -INFINITY ? 0.f : m[nt];
@@ -302,51 +311,54 @@ __global__ void __launch_bounds__(kAttendThreads) paged_attend_kernel(const __gr
                     bf[nt][e] = transpose8x8(two_terms(pj * f));
                 }
             }
+            // ldmatrix.trans on pairs of bytes: a lane gets the columns 16 c + 2g, + 1 of positions 2t, 2t + 1 (and 8 further on), rows g and g + 8 of tile c
+            const int l_row = u * kPageBlock + (lane & 15), l_c = lane >> 4;       // the row this lane addresses, and its chunk of the two in a load
 #pragma unroll
-            for (int w = 0; w < VW; ++w) {
-                // pairs of positions for four columns of the output: rows g and g + 8 of two tiles
-                const uint32_t y0 = biased<FMT>(vw[u][0][w]), y1 = biased<FMT>(vw[u][1][w]), y2 = biased<FMT>(vw[u][2][w]), y3 = biased<FMT>(vw[u][3][w]);
-                const uint32_t lo01 = __byte_perm(y0, y1, 0x5140), hi01 = __byte_perm(y0, y1, 0x7362);
-                const uint32_t lo23 = __byte_perm(y2, y3, 0x5140), hi23 = __byte_perm(y2, y3, 0x7362);
-                const uint32_t a[2][4] = {{pair16<FMT>(lo01, false), pair16<FMT>(lo01, true), pair16<FMT>(lo23, false), pair16<FMT>(lo23, true)},
-                                          {pair16<FMT>(hi01, false), pair16<FMT>(hi01, true), pair16<FMT>(hi23, false), pair16<FMT>(hi23, true)}};
+            for (int c = 0; c < MT; c += 2) {
+                uint32_t v[4];
+                ldmatrix_trans(v, st + S::kV + l_row * D + v_chunk<D>(l_row, c + l_c) * 16);
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t y0 = biased<FMT>(v[2 * x]), y1 = biased<FMT>(v[2 * x + 1]);
+                    const uint32_t a0 = across16<FMT>(y0, false), a1 = across16<FMT>(y0, true), a2 = across16<FMT>(y1, false), a3 = across16<FMT>(y1, true);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][2 * w + x], a[x][0], a[x][1], a[x][2], a[x][3], bf[nt][0], bf[nt][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + x], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
+                }
             }
         }
-        if (more) load_v(i + 1, id);
     }
 
-    // warps joined
+    // warps joined, in the memory of the rings
+    cp_wait<0>();
+    __syncthreads();
+    float* s_o = reinterpret_cast<float*>(smem);          // [warps][H][D]
+    float* s_m = s_o + kAttendWarps * H * D;              // [warps][H]
+    float* s_l = s_m + kAttendWarps * H;
     const float down = pow2(max(r_exp - 13, -126));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) l[nt] += __shfl_xor_sync(0xffffffffu, l[nt], off);
-        const int j = nt * 4 + t;
-        if (g == 0) { s_m[warp][j] = m[nt]; s_l[warp][j] = l[nt]; }
+        const int j = warp * H + nt * 4 + t;
+        if (g == 0) { s_m[j] = m[nt]; s_l[j] = l[nt]; }
 #pragma unroll
-        for (int w = 0; w < VW; ++w)
-            *reinterpret_cast<float4*>(&s_o[warp][j][v_col + 4 * w]) =
-                make_float4((o[nt][2 * w][0] + o[nt][2 * w][1]) * down, (o[nt][2 * w][2] + o[nt][2 * w][3]) * down,
-                            (o[nt][2 * w + 1][0] + o[nt][2 * w + 1][1]) * down, (o[nt][2 * w + 1][2] + o[nt][2 * w + 1][3]) * down);
+        for (int c = 0; c < MT; ++c)
+            *reinterpret_cast<float2*>(s_o + j * D + 16 * c + 2 * g) = make_float2((o[nt][c][0] + o[nt][c][1]) * down, (o[nt][c][2] + o[nt][c][3]) * down);
     }
     __syncthreads();
     for (int e = tid; e < nh * (D / 4); e += kAttendThreads) {
         const int j = e / (D / 4), x = e % (D / 4) * 4;
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kAttendWarps; ++w) mx = fmaxf(mx, s_m[w][j]);
+        for (int w = 0; w < kAttendWarps; ++w) mx = fmaxf(mx, s_m[w * H + j]);
         const float ref = mx == -INFINITY ? 0.f : mx;
         float den = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kAttendWarps; ++w) {
-            const float f = __expf(s_m[w][j] - ref);
-            const float4 v = *reinterpret_cast<const float4*>(&s_o[w][j][x]);
-            den = fmaf(f, s_l[w][j], den);
+            const float f = __expf(s_m[w * H + j] - ref);
+            const float4 v = *reinterpret_cast<const float4*>(s_o + (w * H + j) * D + x);
+            den = fmaf(f, s_l[w * H + j], den);
             acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
         }
         if (parts == 1) {
@@ -386,23 +398,28 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
 
 // ------------------------------------------------------------------ launches
 constexpr int kMinTiles = kUnit * kAttendWarps;           // of a CTA: less would leave warps without work
-constexpr int kSlots = 4;                                 // CTAs an SM is given at least, as long as there are tiles
+constexpr int kSplitCtas = 8;                             // CTAs an SM is given at most by splitting
 
 int column_tiles(int G) { return G > 4 ? 2 : 1; }
-
-int splits_for(int64_t ctas, int tiles) {
-    const int64_t want = (int64_t)sm_count() * kSlots;
-    if (ctas >= want) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((want + ctas - 1) / ctas, (tiles + kMinTiles - 1) / kMinTiles));
-}
-
 int head_passes(int G) { return (G + 4 * column_tiles(G) - 1) / (4 * column_tiles(G)); }
 
-// Parts that a step may produce, times heads: with B * Hkv * passes CTAs below `want`, fewer than twice as many after splitting.
+// CTAs a sequence is split over: what per_sm CTAs an SM take in whole waves, counted in tiles, each CTA with the cost of its start and end, and the merge.
+int splits_for(int64_t ctas, int tiles, int per_sm, bool given) {
+    const int64_t slots = per_sm * (int64_t)sm_count(), most = std::min<int64_t>((tiles + kMinTiles - 1) / kMinTiles, kSplitCtas * (int64_t)sm_count() / ctas);
+    const int64_t start = given ? 16 : 10, merge = given ? 32 : 16;
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t s = 1; s <= std::max<int64_t>(1, most); ++s) {
+        const int64_t each = ((tiles + s - 1) / s + kMinTiles - 1) / kMinTiles * kMinTiles;
+        const int64_t cost = (ctas * s + slots - 1) / slots * (each + start) + (s > 1 ? merge : 0);
+        if (cost < least) { least = cost; best = s; }
+    }
+    return (int)best;
+}
+
+// Room for the parts of a step: splitting makes no more than kSplitCtas CTAs an SM, of 4 or 8 heads each, and none below kMinTiles tiles.
 size_t part_bytes(int B, int Hq, int Hkv, int d, int L) {
-    const int G = Hq / Hkv;
     const int64_t tiles = (L + kPageBlock - 1) / kPageBlock;
-    const int64_t most = 2 * (int64_t)sm_count() * kSlots * 4 * column_tiles(G), all = (int64_t)B * Hq * ((tiles + kMinTiles - 1) / kMinTiles);
+    const int64_t most = kSplitCtas * (int64_t)sm_count() * 4 * column_tiles(Hq / Hkv), all = (int64_t)B * Hq * ((tiles + kMinTiles - 1) / kMinTiles);
     const size_t n = ((size_t)std::min(most, all) + 3) & ~(size_t)3;
     return (n * (2 + (size_t)d) * sizeof(float) + 255) & ~(size_t)255;
 }
@@ -413,20 +430,22 @@ cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
     p.heads = 4 * nt;
     p.passes = head_passes(p.G);
     const int64_t ctas = (int64_t)p.B * p.pool.Hkv * p.passes;
-    const int splits = splits_for(ctas, all_tiles);
+    const int splits = splits_for(ctas, all_tiles, nt == 2 ? Stage<128, 8, GIVEN>::kCtas : Stage<128, 4, GIVEN>::kCtas, GIVEN);
     p.tiles = ((all_tiles + splits - 1) / splits + kMinTiles - 1) / kMinTiles * kMinTiles;
     p.splits = (all_tiles + p.tiles - 1) / p.tiles;
-    const size_t n = ((size_t)p.B * p.splits * p.Hq + 3) & ~(size_t)3;
+    const size_t n = ((size_t)p.B * p.splits * p.Hq + 3) & ~(size_t)3;     // (not used where nothing is split)
     p.ws_m = static_cast<float*>(ws);
     p.ws_l = p.ws_m + n;
     p.ws_o = p.ws_l + n;
-    void (*kernel)(AttendParams) = nullptr;
-    switch (p.pool.d) {
-        case 128: kernel = nt == 2 ? paged_attend_kernel<FMT, 128, 2, GIVEN> : paged_attend_kernel<FMT, 128, 1, GIVEN>; break;
-        case 64: kernel = nt == 2 ? paged_attend_kernel<FMT, 64, 2, GIVEN> : paged_attend_kernel<FMT, 64, 1, GIVEN>; break;
-        default: kernel = nt == 2 ? paged_attend_kernel<FMT, 32, 2, GIVEN> : paged_attend_kernel<FMT, 32, 1, GIVEN>; break;
-    }
-    cudaError_t e = launch_chained(kernel, dim3(p.splits, p.pool.Hkv * p.passes, p.B), dim3(kAttendThreads), 0, s, p);
+    auto attend = [&](auto width) -> cudaError_t {
+        constexpr int D = decltype(width)::value;
+        void (*kernel)(AttendParams) = nt == 2 ? paged_attend_kernel<FMT, D, 2, GIVEN> : paged_attend_kernel<FMT, D, 1, GIVEN>;
+        const size_t smem = nt == 2 ? Stage<D, 8, GIVEN>::kTotal : Stage<D, 4, GIVEN>::kTotal;
+        const cudaError_t e = allow_smem(kernel, smem, true);
+        return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.splits, p.pool.Hkv * p.passes, p.B), dim3(kAttendThreads), smem, s, p);
+    };
+    cudaError_t e = p.pool.d == 128 ? attend(std::integral_constant<int, 128>{}) : p.pool.d == 64 ? attend(std::integral_constant<int, 64>{})
+                                                                                                    : attend(std::integral_constant<int, 32>{});
     count_launches(1);
     if (e != cudaSuccess || p.splits == 1) return e;
     e = launch_chained(paged_merge_kernel, dim3(p.Hq, p.B), dim3(128), 0, s, p);
