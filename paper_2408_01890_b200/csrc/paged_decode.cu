@@ -60,16 +60,6 @@ struct Stage {
     static constexpr int kCtas = H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
 };
 
-// 16, 8 or 4 bytes from global to shared memory, zeros where !ok (nothing is read then)
-template <int N>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) {
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(ok ? N : 0), "n"(N) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // Rows lie with their 16-byte chunks permuted, so that the eight lanes of a shared-memory access meet eight different ones.  A K access is four
 // chunks of two neighbouring rows; a V access (ldmatrix) one chunk of eight rows, of which 64- and 32-byte rows put two and four beside one another.
 template <int D>

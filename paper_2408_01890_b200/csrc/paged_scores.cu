@@ -104,114 +104,123 @@ size_t general_smem(const ScoresParams& p) {
 // ---------------------------------------------------------------------------------------------
 // 32 or 40 heads, bf16 weights, hidden widths that are multiples of 8 up to 256, adding or concatenating Integrate
 // ---------------------------------------------------------------------------------------------
-constexpr int kScoresThreads = 256;
-constexpr int kScoresWarps = kScoresThreads / 32;
+constexpr int kRingHeads = 3;            // KV heads' K' of a warp on their way or in use
 
-// Shared memory of a CTA (byte offsets): differences [HQ][CH + 4], partial FFN outputs [HS][HQ][CH + 4] (HS > 1), q' [HQ][32] and its scales, weights, biases
+// Shared memory of a CTA (byte offsets): differences [HQ][CH + 4], partial FFN outputs [HS][HQ][CH + 4] (HS > 1), the two terms of q' [HQ][2][32] and its
+// scales, weights, biases, and the warps' rings: a stage is [CH / 16 blocks][24 or 32 ranks][16 positions] and the blocks' scales
 struct ScoresLayout {
-    int y, qp, q_scale, w1, w2, b1, b2, total;
+    int y, qp, q_scale, w1, w2, b1, b2, ring, stage, scales, total;
 };
-__host__ __device__ inline ScoresLayout scores_layout(int HQ, int CH, bool concat, int m) {
+__host__ __device__ inline ScoresLayout scores_layout(int HQ, int NW, int CH, bool concat, int m, int r) {
     ScoresLayout l;
-    const int HS = 128 / CH, mp = (m + 15) / 16 * 16, kp = concat ? 2 * HQ : (HQ + 15) / 16 * 16;
+    const int HS = NW * 16 / CH, mp = (m + 15) / 16 * 16, kp = concat ? 2 * HQ : (HQ + 15) / 16 * 16;
     int off = HQ * (CH + 4) * 4;
     l.y = off; off += HS > 1 ? HS * HQ * (CH + 4) * 4 : 0;
-    l.qp = off; off += HQ * kMaxRank * 4;
+    l.qp = off; off += HQ * 2 * kMaxRank * 2;
     l.q_scale = off; off += HQ * 4;
     l.w1 = off; off += kp * (mp + 8) * 2;
     l.w2 = off; off += mp * (HQ + 8) * 2;
     l.b1 = off; off += mp * 4;
     l.b2 = off; off += HQ * 4;
-    l.total = off;
+    l.ring = off;
+    l.scales = CH / kPageBlock * (r > 24 ? 32 : 24) * 16 + (r > 24 ? 0 : 128);      // (the load of a block of 24 ranks reaches 8 further)
+    l.stage = l.scales + (CH / kPageBlock * 8 + 15) / 16 * 16;
+    l.total = off + NW * kRingHeads * l.stage;
     return l;
 }
 
-// Differences of one KV head's up to four query heads h0 .. h0 + nh - 1 at the 16 positions of this lane's block
-template <int FMT>
-__device__ __forceinline__ void delta_blocks(const PagedView& pool, const uint8_t* page, int pos, int kvh, int h0, int nh, bool on, const float* qp_s,
-                                             const float* q_scale, float* s_s, int ld) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r = pool.r;
-    const uint8_t* at = page + pool.kp_block(kvh, pos) + t * kPageBlock;
-    uint32_t w[2][4][4];
+// Differences of up to four query heads of one KV head, whose K' lies in a stage: positions 2g and 2g + 1 of a block are rows g and g + 8, ranks are k
+template <int FMT, int NB>
+__device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, bool wide, const __half* q, const float* q_scale, int nh, float* s_s, int ld) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, ranks = wide ? 32 : 24;
+    // column g: head g / 2's leading (even g) or second term
+    uint32_t bf[4];
+    const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (g >> 1) * 2 * kMaxRank + (g & 1) * kMaxRank) + t;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int i = 0; i < 4; ++i) bf[i] = (g >> 1) < nh && (wide || i < 3) ? qr[4 * i] : 0u;
+    const float qs = t < nh ? q_scale[t] : 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 v = ld_stream16_or_zero(at + (16 * s + 4 * i) * kPageBlock, on && 16 * s + 4 * i + t < r);
-            w[s][i][0] = v.x; w[s][i][1] = v.y; w[s][i][2] = v.z; w[s][i][3] = v.w;
-        }
-    const float scale = on ? pool.scales(const_cast<uint8_t*>(page), kvh, pos)[0] : 0.f;
-    // column g: head g / 2's leading (even g) or second term; k-step s: ranks 16 s + 4 i + t
-    uint32_t bf[2][2];
+    for (int k = 0; k < NB; ++k) {
+        uint32_t w[4];
+        ldmatrix_trans(w, stage + (k * ranks + lane) * 16);
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float* q = qp_s + (h0 + (g >> 1)) * kMaxRank + 16 * s + 8 * e + t;
-            bf[s][e] = (g >> 1) < nh ? pack16(term_of(q[0], g & 1), term_of(q[4], g & 1)) : 0u;
-        }
-    float c[8][4];
-#pragma unroll
-    for (int mt = 0; mt < 8; ++mt) c[mt][0] = c[mt][1] = c[mt][2] = c[mt][3] = 0.f;
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t y0 = biased<FMT>(w[s][0][k]), y1 = biased<FMT>(w[s][1][k]), y2 = biased<FMT>(w[s][2][k]), y3 = biased<FMT>(w[s][3][k]);
-            const uint32_t lo01 = __byte_perm(y0, y1, 0x5140), hi01 = __byte_perm(y0, y1, 0x7362);
-            const uint32_t lo23 = __byte_perm(y2, y3, 0x5140), hi23 = __byte_perm(y2, y3, 0x7362);
-            mma_f16(c[2 * k], pair16<FMT>(lo01, false), pair16<FMT>(lo01, true), pair16<FMT>(lo23, false), pair16<FMT>(lo23, true), bf[s][0], bf[s][1]);
-            mma_f16(c[2 * k + 1], pair16<FMT>(hi01, false), pair16<FMT>(hi01, true), pair16<FMT>(hi23, false), pair16<FMT>(hi23, true), bf[s][0], bf[s][1]);
-        }
-    if (t >= nh || !on) return;
-    const float f = scale * q_scale[h0 + t];
-    float4* dst = reinterpret_cast<float4*>(s_s + (h0 + t) * ld + g * kPageBlock);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        dst[k] = make_float4((c[2 * k][0] + c[2 * k][1]) * f, (c[2 * k][2] + c[2 * k][3]) * f, (c[2 * k + 1][0] + c[2 * k + 1][1]) * f,
-                             (c[2 * k + 1][2] + c[2 * k + 1][3]) * f);
+        for (int i = 0; i < 4; ++i) w[i] = biased<FMT>(w[i]);
+        mma_f16(c, across16<FMT>(w[0], false), across16<FMT>(w[0], true), across16<FMT>(w[1], false), across16<FMT>(w[1], true), bf[0], bf[1]);
+        if (wide) mma_f16(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), across16<FMT>(w[3], false), across16<FMT>(w[3], true), bf[2], bf[3]);
+        else mma_f16_k8(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), bf[2]);
+        const float f = reinterpret_cast<const float2*>(stage + scales)[k].x * qs;
+        if (t < nh) *reinterpret_cast<float2*>(s_s + t * ld + k * kPageBlock + 2 * g) = make_float2((c[0] + c[1]) * f, (c[2] + c[3]) * f);
+    }
 }
 
-template <int HQ, int CH, bool CONCAT>
-__global__ void __launch_bounds__(kScoresThreads, 2) paged_scores_kernel(const __grid_constant__ ScoresParams p, int dtype) {
-    constexpr int HS = 128 / CH, LD = CH + 4, NT2 = HQ / 8, KPH = (HQ + 15) / 16, KS1 = CONCAT ? 2 * HQ / 16 : KPH, W2_LD = HQ + 8;
+template <int HQ, int NW, int CH, bool CONCAT>
+__global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(const __grid_constant__ ScoresParams p, int dtype) {
+    constexpr int THREADS = NW * 32, HS = NW * 16 / CH, LD = CH + 4, NB = CH / kPageBlock, NT2 = HQ / 8, KPH = (HQ + 15) / 16;
+    constexpr int KS1 = CONCAT ? 2 * HQ / 16 : KPH, W2_LD = HQ + 8;
     extern __shared__ __align__(16) uint8_t smem_b[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int b = blockIdx.y, j0 = blockIdx.x * CH, m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8;
-    const ScoresLayout lay = scores_layout(HQ, CH, CONCAT, m);
+    const int b = blockIdx.y, j0 = blockIdx.x * CH, m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8, r = p.pool.r;
+    const ScoresLayout lay = scores_layout(HQ, NW, CH, CONCAT, m, r);
     float* s_s = reinterpret_cast<float*>(smem_b);
     float* y_s = reinterpret_cast<float*>(smem_b + lay.y);
-    float* qp_s = reinterpret_cast<float*>(smem_b + lay.qp);
+    __half* qp_s = reinterpret_cast<__half*>(smem_b + lay.qp);
     float* q_scale = reinterpret_cast<float*>(smem_b + lay.q_scale);
     __nv_bfloat16* w1_s = reinterpret_cast<__nv_bfloat16*>(smem_b + lay.w1);     // [inputs][mp + 8], zero rows and columns beyond the FFN's sizes
     __nv_bfloat16* w2_s = reinterpret_cast<__nv_bfloat16*>(smem_b + lay.w2);     // [mp][HQ + 8]
     float* b1_s = reinterpret_cast<float*>(smem_b + lay.b1);
     float* b2_s = reinterpret_cast<float*>(smem_b + lay.b2);
+    uint8_t* ring = smem_b + lay.ring + warp * kRingHeads * lay.stage;
     chain_release();
     // the aligner's weights are constants of the model: staged while the kernel before this one may still be running
     const int c8 = mp / 8;
-    for (int e = tid; e < KS1 * 16 * c8; e += kScoresThreads) {
+    for (int e = tid; e < KS1 * 16 * c8; e += THREADS) {
         const int k = e / c8, c = (e - k * c8) * 8;
-        *reinterpret_cast<uint4*>(w1_s + k * w1_ld + c) = k < (CONCAT ? 2 * HQ : HQ) && c < m
-            ? *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.w1) + k * m + c) : make_uint4(0u, 0u, 0u, 0u);
+        const bool in = k < (CONCAT ? 2 * HQ : HQ) && c < m;
+        cp_async<16>((uint32_t)__cvta_generic_to_shared(w1_s + k * w1_ld + c), static_cast<const __nv_bfloat16*>(p.w1) + (in ? k * m + c : 0), in);
     }
-    for (int e = tid; e < mp * NT2; e += kScoresThreads) {
+    for (int e = tid; e < mp * NT2; e += THREADS) {
         const int k = e / NT2, c = e % NT2 * 8;
-        *reinterpret_cast<uint4*>(w2_s + k * W2_LD + c) = k < m
-            ? *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.w2) + k * HQ + c) : make_uint4(0u, 0u, 0u, 0u);
+        cp_async<16>((uint32_t)__cvta_generic_to_shared(w2_s + k * W2_LD + c), static_cast<const __nv_bfloat16*>(p.w2) + (k < m ? k * HQ + c : 0), k < m);
     }
-    for (int e = tid; e < mp; e += kScoresThreads) b1_s[e] = e < m ? ldw(p.b1, e, p.w_dtype) : 0.f;
-    for (int e = tid; e < HQ; e += kScoresThreads) b2_s[e] = ldw(p.b2, e, p.w_dtype);
+    cp_commit();
+    for (int e = tid; e < mp; e += THREADS) b1_s[e] = e < m ? ldw(p.b1, e, p.w_dtype) : 0.f;
+    for (int e = tid; e < HQ; e += THREADS) b2_s[e] = ldw(p.b2, e, p.w_dtype);
+    for (int e = lane; e < kRingHeads * lay.stage / 16; e += 32) reinterpret_cast<uint4*>(ring)[e] = make_uint4(0u, 0u, 0u, 0u);   // ranks beyond r stay zero
+    __syncwarp();
     chain_wait();
     const int L = length_of(p.seq_lens, b, p.L);
-    if (j0 >= L) return;
+    if (j0 >= L) {
+        cp_wait<0>();
+        return;
+    }
 
-    // this lane's block of the chunk
-    const int blk_pos = j0 + g * kPageBlock;
-    const int id = g < CH / kPageBlock && blk_pos < L ? p.pool.page_of(b, blk_pos, warp == 0 && t == 0) : -1;
-    const uint8_t* page = p.pool.page(max(id, 0));
+    // lane i: page of the chunk's block i
+    const int id = lane < NB && j0 + lane * kPageBlock < L ? p.pool.page_of(b, j0 + lane * kPageBlock, warp == 0) : -1;
+    const uint32_t there = __ballot_sync(0xffffffffu, id >= 0);
+    const uint8_t* kp_at[NB];             // this lane's rank of KV head 0 in each block
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+        kp_at[k] = p.pool.page(max(__shfl_sync(0xffffffffu, id, k), 0)) + p.pool.kp_block(0, j0 + k * kPageBlock) + lane * kPageBlock;
+    const uint8_t* scale_at = reinterpret_cast<const uint8_t*>(p.pool.scales(p.pool.page(max(id, 0)), 0, j0 + lane * kPageBlock));
+    const int blocks = 1 << (p.pool.shift - 4), passes = (p.G + 3) / 4, n_kv = p.pool.Hkv;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    auto ask = [&](int kvh, int stage) {
+        if (kvh < n_kv) {
+            const uint32_t to = ring_at + stage * lay.stage;
+            const int64_t head = (int64_t)kvh * blocks;
+#pragma unroll
+            for (int k = 0; k < NB; ++k)
+                if (lane < r) cp_async<16>(to + (k * (r > 24 ? 32 : 24) + lane) * 16, kp_at[k] + head * (r * kPageBlock), there >> k & 1);
+            if (lane < NB) cp_async<8>(to + lay.scales + lane * 8, scale_at + head * 8, id >= 0);
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kRingHeads - 1; ++i) ask(warp + i * NW, i);
+
     // the previous scores of the FFN phase: asked for now
-    const int strip = warp % (CH / 16), hs = warp / (CH / 16), p0 = strip * 16 + g, p1 = p0 + 8;
+    const int strip = warp % NB, hs = warp / NB, p0 = strip * 16 + g, p1 = p0 + 8;
     const bool ok0 = j0 + p0 < L, ok1 = j0 + p1 < L;
     float pv[KPH * 4][2];               // slots 2 i, 2 i + 1: heads 8 i + 2t, + 1
     auto load_prev = [&](const auto* row) {
@@ -230,22 +239,30 @@ __global__ void __launch_bounds__(kScoresThreads, 2) paged_scores_kernel(const _
     if (p.row_bf16) load_prev(static_cast<const __nv_bfloat16*>(p.prev));
     else load_prev(static_cast<const float*>(p.prev));
 
-    // q', each head brought to [2^13, 2^14) by a power of two
-    for (int h = warp; h < HQ; h += kScoresWarps) {
-        const float x = lane < p.pool.r ? ld_elem(p.qp.ptr, b * p.qp.sb + h * p.qp.sh + lane, p.qp.dtype) : 0.f;
+    // q', each head brought to [2^13, 2^14) by a power of two, as two fp16 terms
+    for (int h = warp; h < HQ; h += NW) {
+        float x = lane < r ? ld_elem(p.qp.ptr, b * p.qp.sb + h * p.qp.sh + lane, p.qp.dtype) : 0.f;
         const int ex = exponent(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu)));
-        qp_s[h * kMaxRank + lane] = x * pow2(13 - ex);
-        if (lane == 0) q_scale[h] = pow2(ex - 13) * rsqrtf((float)p.pool.r);
+        x *= pow2(13 - ex);
+        const __half hi = __float2half_rn(x);
+        qp_s[h * 2 * kMaxRank + lane] = hi;
+        qp_s[h * 2 * kMaxRank + kMaxRank + lane] = __float2half_rn(x - __half2float(hi));
+        if (lane == 0) q_scale[h] = pow2(ex - 13) * rsqrtf((float)r);
     }
-    if (CH < 128 || j0 + CH > L)        // absent blocks: their differences are zeros
-        for (int e = tid; e < HQ * LD; e += kScoresThreads) s_s[e] = 0.f;
     __syncthreads();
-    const int passes = (p.G + 3) / 4, nv = p.pool.Hkv * passes;
-    for (int v = warp; v < nv; v += kScoresWarps) {
-        const int kvh = v / passes, q0 = v % passes * 4, nh = min(4, p.G - q0);
-        if (dtype == LISA_S8) delta_blocks<LISA_S8>(p.pool, page, blk_pos, kvh, kvh * p.G + q0, nh, id >= 0, qp_s, q_scale, s_s, LD);
-        else delta_blocks<LISA_E4M3>(p.pool, page, blk_pos, kvh, kvh * p.G + q0, nh, id >= 0, qp_s, q_scale, s_s, LD);
+
+    // phase 1
+    for (int kvh = warp, stage = 0; kvh < n_kv; kvh += NW, stage = stage + 1 == kRingHeads ? 0 : stage + 1) {
+        cp_wait<kRingHeads - 2>();
+        __syncwarp();
+        ask(kvh + (kRingHeads - 1) * NW, stage == 0 ? kRingHeads - 1 : stage - 1);
+        for (int pass = 0; pass < passes; ++pass) {
+            const int h0 = kvh * p.G + pass * 4, nh = min(4, p.G - pass * 4);
+            if (dtype == LISA_S8) delta_blocks<LISA_S8, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + h0 * 2 * kMaxRank, q_scale + h0, nh, s_s + h0 * LD, LD);
+            else delta_blocks<LISA_E4M3, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + h0 * 2 * kMaxRank, q_scale + h0, nh, s_s + h0 * LD, LD);
+        }
     }
+    cp_wait<0>();                         // (the weights; a warp without heads has not waited)
     __syncthreads();
 
     // the FFN: a warp owns 16 positions and every HS-th block of 16 hidden units
@@ -314,15 +331,18 @@ __global__ void __launch_bounds__(kScoresThreads, 2) paged_scores_kernel(const _
     }
     // yacc[j]: [0] (p0, head 8 j + 2t), [1] (p0, + 1), [2] (p1, 2t), [3] (p1, + 1)
     if constexpr (HS == 1) {
-        // whether a position's page is there is known to the lanes that hold its block: lanes 4 strip .. 4 strip + 3
-        const bool there = __shfl_sync(0xffffffffu, id, 4 * strip) >= 0;
-        if (!there) return;
+        if (!(there >> strip & 1)) return;
+        const bool also = p.out_scores;
+        float* to = p.scores + b * p.s_sb + 2 * t * p.s_sh + j0;
 #pragma unroll
         for (int j = 0; j < NT2; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int h = j * 8 + 2 * t + (e & 1), pos = e & 2 ? p1 : p0;
-                if (e & 2 ? ok1 : ok0) put_score(p, b, h, j0 + pos, yacc[j][e] + (CONCAT ? 0.f : s_s[h * LD + pos]));
+                const int h = j * 8 + (e & 1), pos = e & 2 ? p1 : p0;
+                const float v = yacc[j][e] + (CONCAT ? 0.f : s_s[(h + 2 * t) * LD + pos]);
+                if (!(e & 2 ? ok1 : ok0)) continue;
+                if (also) put_score(p, b, h + 2 * t, j0 + pos, v);
+                else to[h * p.s_sh + pos] = v;
             }
     } else {
 #pragma unroll
@@ -330,11 +350,9 @@ __global__ void __launch_bounds__(kScoresThreads, 2) paged_scores_kernel(const _
 #pragma unroll
             for (int e = 0; e < 4; ++e) y_s[(hs * HQ + j * 8 + 2 * t + (e & 1)) * LD + (e & 2 ? p1 : p0)] = yacc[j][e];
         __syncthreads();
-        // pages of the chunk's blocks: lane 4 i holds block i's
-        const uint32_t there = __ballot_sync(0xffffffffu, id >= 0);
-        for (int e = tid; e < HQ * CH; e += kScoresThreads) {
+        for (int e = tid; e < HQ * CH; e += THREADS) {
             const int h = e / CH, pos = e % CH;
-            if (j0 + pos >= L || !(there >> (pos / kPageBlock * 4) & 1)) continue;
+            if (j0 + pos >= L || !(there >> (pos / kPageBlock) & 1)) continue;
             float x = CONCAT ? 0.f : s_s[h * LD + pos];
 #pragma unroll
             for (int q = 0; q < HS; ++q) x += y_s[(q * HQ + h) * LD + pos];
@@ -345,14 +363,18 @@ __global__ void __launch_bounds__(kScoresThreads, 2) paged_scores_kernel(const _
 
 template <int HQ, bool CONCAT>
 cudaError_t launch_fast(const ScoresParams& p, int dtype, cudaStream_t s) {
-    // 128 positions to a CTA once that gives every SM one, else fewer
-    int ch = 128;
-    while (ch > 16 && (int64_t)p.B * ((p.L + ch - 1) / ch) < sm_count()) ch /= 2;
-    auto kernel = ch == 128 ? paged_scores_kernel<HQ, 128, CONCAT> : ch == 64 ? paged_scores_kernel<HQ, 64, CONCAT>
-                : ch == 32 ? paged_scores_kernel<HQ, 32, CONCAT> : paged_scores_kernel<HQ, 16, CONCAT>;
-    const size_t smem = (size_t)scores_layout(HQ, ch, CONCAT, p.m).total;
-    const cudaError_t e = allow_smem(kernel, smem);
-    return e != cudaSuccess ? e : launch_chained(kernel, dim3((p.L + ch - 1) / ch, p.B), dim3(kScoresThreads), smem, s, p, dtype);
+    // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128.  Fewer positions where that
+    // does not give every SM two CTAs.
+    constexpr int NW = CONCAT ? 8 : 4;
+    int ch = NW * 16;
+    while (ch > 16 && (int64_t)p.B * ((p.L + ch - 1) / ch) < 2 * (int64_t)sm_count()) ch /= 2;
+    void (*kernel)(ScoresParams, int) = ch == 64 ? paged_scores_kernel<HQ, NW, 64, CONCAT> : ch == 32 ? paged_scores_kernel<HQ, NW, 32, CONCAT>
+                                                                                          : paged_scores_kernel<HQ, NW, 16, CONCAT>;
+    if constexpr (CONCAT)
+        if (ch == 128) kernel = paged_scores_kernel<HQ, NW, 128, CONCAT>;
+    const size_t smem = (size_t)scores_layout(HQ, NW, ch, CONCAT, p.m, p.pool.r).total;
+    const cudaError_t e = allow_smem(kernel, smem, true);
+    return e != cudaSuccess ? e : launch_chained(kernel, dim3((p.L + ch - 1) / ch, p.B), dim3(NW * 32), smem, s, p, dtype);
 }
 
 bool vec16(const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0; }
