@@ -56,7 +56,8 @@ struct Stage {
     static constexpr int kCount = GIVEN ? 3 : 2;
     static constexpr int kRing = kBytes * kCount;
     static constexpr int kMerge = kAttendWarps * H * (D + 2) * 4;
-    static constexpr int kTotal = kRing * kAttendWarps > kMerge ? kRing * kAttendWarps : kMerge;
+    static constexpr int kQuery = (kRing * kAttendWarps > kMerge ? kRing * kAttendWarps : kMerge);     // the queries as operands, behind the rings
+    static constexpr int kTotal = kQuery + (GIVEN ? 0 : H * (4 * D + 4));
     static constexpr int kCtas = H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
 };
 
@@ -66,6 +67,19 @@ template <int D>
 __device__ __forceinline__ int k_chunk(int row, int c) { return D == 128 ? c ^ ((row & 1) << 2) : c; }
 template <int D>
 __device__ __forceinline__ int v_chunk(int row, int c) { return c ^ (D == 128 ? row & 7 : D == 64 ? row >> 1 & 3 : row >> 2 & 1); }
+
+constexpr float kLog2e = 1.4426950408889634f;             // scores are kept times this, so that exponentials are powers of two
+__device__ __forceinline__ float exp2_(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void put_row(const AttendParams& p, int b, int h, int pos, float v) {
+    const int64_t to = b * p.sc_sb + h * p.sc_sh + pos;
+    if (p.row_bf16) st_row<true>(p.out_scores, to, v);
+    else st_row<false>(p.out_scores, to, v);
+}
 
 template <int W>
 __device__ __forceinline__ void lds_words(uint32_t* w, const uint8_t* p) {
@@ -80,13 +94,431 @@ __device__ __forceinline__ void lds_words(uint32_t* w, const uint8_t* p) {
     }
 }
 
+// Rows g and g + 8 of tile u of a stage, 4 D / 128 ... words of each; the columns of word w are k_column .. + 3
+template <int D>
+__device__ __forceinline__ int k_column(int w, int t) { return D == 128 ? (w >> 2) * 64 + 16 * t + 4 * (w & 3) : D / 4 * t + 4 * w; }
+template <int D>
+__device__ __forceinline__ void load_k(uint32_t (*kw)[D / 16], const uint8_t* st, int u) {
+    constexpr int KW = D / 16, W = KW < 4 ? KW : 4;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int row = u * kPageBlock + g + 8 * e;
+#pragma unroll
+        for (int x = 0; x < KW / W; ++x) lds_words<W>(&kw[e][x * W], st + row * D + (D == 128 ? k_chunk<D>(row, 4 * x + t) * 16 : 4 * KW * t));
+    }
+}
+// Chunks c and c + 1 of tile u of V, transposed as pairs of bytes: v[2 x], v[2 x + 1] hold columns 16 (c + x) + 2g, + 1 of positions 2t, 2t + 1 and of 2t + 8,
+// 2t + 9: as A operand of a product over positions, rows g and g + 8 of the tile of columns c + x
+template <int D>
+__device__ __forceinline__ void load_v(uint32_t* v, const uint8_t* rows, int u, int c) {
+    const int lane = threadIdx.x & 31, row = u * kPageBlock + (lane & 15);
+    ldmatrix_trans(v, rows + row * D + v_chunk<D>(row, c + (lane >> 4)) * 16);
+}
+
+// This lane's D / 32 values of a query, and the largest magnitude of all (a NaN or an infinity being the largest)
+template <int D>
+__device__ __forceinline__ float query_of(float* x, const AttendParams& p, int b, int h, bool on) {
+    const int64_t at = b * p.q.sb + h * p.q.sh + (threadIdx.x & 31) * (D / 32);
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+        x[e] = on ? ld_elem(p.q.ptr, at + e, p.q.dtype) : 0.f;
+        amax = max(amax, __float_as_uint(x[e]) & 0x7fffffffu);
+    }
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, amax));
+}
+
+// The arithmetic of a warp over its units.  Shared memory of a stage: st; pos0: the unit's first position; there: bit u: tile u's page is there.
+//
+// e4m3: products on mma m16n8k16 fp16, where every code is exact; the other operand as two fp16 terms, so that the eight columns are four heads.
+template <int D, int NT, bool GIVEN>
+struct EngineF16 {
+    static constexpr int H = 4 * NT, KW = D / 16, MT = D / 16;   // words of a lane per K row; tiles of 16 output columns
+    using S = Stage<D, H, GIVEN>;
+    uint32_t qf[GIVEN ? 1 : NT][KW][2];
+    float q_scale[NT], m[NT], l[NT], o[NT][MT][4];               // m, l, q_scale: of head t
+    int r_exp;                                                    // V enters as code * 2^12 scale / 2^r_exp
+
+    __device__ __forceinline__ void start(const uint8_t* q_s) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        r_exp = kLeastExp;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt] = -INFINITY;
+            l[nt] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][mt][e] = 0.f;
+        }
+        if constexpr (!GIVEN) {   // column g is head g / 2's leading (even g) or second term
+            const __half* q = reinterpret_cast<const __half*>(q_s);
+            const float* scale = reinterpret_cast<const float*>(q_s + H * 4 * D);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int j = nt * 4 + (g >> 1);
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(q + (j * 2 + (g & 1)) * D + k_column<D>(w, t));
+                    qf[nt][w][0] = v.x; qf[nt][w][1] = v.y;
+                }
+                q_scale[nt] = scale[nt * 4 + t];
+            }
+        }
+    }
+
+    // The queries' terms [H][2][D] and their scales [H]: a head to a warp, brought to [2^13, 2^14) by a power of two
+    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh) {
+        const int lane = threadIdx.x & 31;
+        for (int j = threadIdx.x >> 5; j < H; j += kAttendWarps) {
+            float x[D / 32];
+            const float amax = query_of<D>(x, p, b, h0 + j, j < nh);
+            const int ex = exponent(amax);
+            const float up = pow2(13 - ex);
+            __half* q = reinterpret_cast<__half*>(q_s) + j * 2 * D + lane * (D / 32);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) {
+                const __half hi = __float2half_rn(x[e] * up);
+                q[e] = hi;
+                q[D + e] = __float2half_rn(x[e] * up - __half2float(hi));
+            }
+            if (lane == 0) reinterpret_cast<float*>(q_s + H * 4 * D)[j] = pow2(ex - 13) * rsqrtf((float)D);
+        }
+    }
+
+    __device__ __forceinline__ void unit(const AttendParams& p, const uint8_t* st, int pos0, int L, int b, int h0, int nh) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        float s[kUnit][NT][2], vs[kUnit];
+        bool there[kUnit];
+#pragma unroll
+        for (int u = 0; u < kUnit; ++u) {
+            const float2 sc = reinterpret_cast<const float2*>(st + S::kScales)[u];
+            vs[u] = sc.y;
+            there[u] = reinterpret_cast<const int*>(st + S::kThere)[u];
+            if constexpr (!GIVEN) {
+                float c[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
+                uint32_t kw[2][KW];
+                load_k<D>(kw, st, u);
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    const uint32_t a0 = pair16<LISA_E4M3>(kw[0][w], false), a1 = pair16<LISA_E4M3>(kw[1][w], false), a2 = pair16<LISA_E4M3>(kw[0][w], true), a3 = pair16<LISA_E4M3>(kw[1][w], true);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(c[nt], a0, a1, a2, a3, qf[nt][w][0], qf[nt][w][1]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float f = sc.x * q_scale[nt];
+                    s[u][nt][0] = (c[nt][0] + c[nt][1]) * f;
+                    s[u][nt][1] = (c[nt][2] + c[nt][3]) * f;
+                }
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int h = nt * 4 + t;
+                        s[u][nt][e] = h < nh ? reinterpret_cast<const float*>(st)[h * kUnitRows + u * kPageBlock + g + 8 * e] : 0.f;
+                    }
+            }
+        }
+        // the reference of the exponentials follows the maximum once it is left behind by a factor of 4
+        bool grown = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int pos = pos0 + u * kPageBlock + g + 8 * e;
+                    const bool on = there[u] && pos < L;
+                    if (!GIVEN && p.out_scores && on && nt * 4 + t < nh) put_row(p, b, h0 + nt * 4 + t, pos, s[u][nt][e]);
+                    s[u][nt][e] = on ? s[u][nt][e] * kLog2e : -INFINITY;
+                    grown |= s[u][nt][e] > m[nt] + 2.f;
+                }
+        if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float mx = m[nt];
+#pragma unroll
+                for (int u = 0; u < kUnit; ++u) mx = fmaxf(mx, fmaxf(s[u][nt][0], s[u][nt][1]));
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                const float f = mx == -INFINITY ? 1.f : exp2_(m[nt] - mx);
+                l[nt] *= f;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
+                m[nt] = mx;
+            }
+        }
+        // V's scales enter with the probabilities; their common power of two follows the largest so far
+        int ex = r_exp;
+#pragma unroll
+        for (int u = 0; u < kUnit; ++u) ex = max(ex, exponent(vs[u]));
+        if (ex > r_exp) {
+            const float f = pow2(max(r_exp - ex, -126));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
+            r_exp = ex;
+        }
+        const float up = pow2(min(12 - r_exp, 127));
+#pragma unroll
+        for (int u = 0; u < kUnit; ++u) {
+            uint32_t bf[NT][2];
+            const float f = vs[u] * up;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float ref = m[nt] == -INFINITY ? 0.f : m[nt];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float pj = exp2_(s[u][nt][e] - ref);
+                    l[nt] += pj;
+                    bf[nt][e] = transpose8x8(two_terms(pj * f));
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < MT; c += 2) {
+                uint32_t v[4];
+                load_v<D>(v, st + S::kV, u, c);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t a0 = across16<LISA_E4M3>(v[2 * x], false), a1 = across16<LISA_E4M3>(v[2 * x], true), a2 = across16<LISA_E4M3>(v[2 * x + 1], false), a3 = across16<LISA_E4M3>(v[2 * x + 1], true);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + x], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
+                }
+            }
+        }
+    }
+
+    // This warp's maximum, sum and output of head j at [j], [j] and [j][D]
+    __device__ __forceinline__ void finish(float* s_m, float* s_l, float* s_o) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const float down = pow2(max(r_exp - 12, -126));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) l[nt] += __shfl_xor_sync(0xffffffffu, l[nt], off);
+            const int j = nt * 4 + t;
+            if (g == 0) { s_m[j] = m[nt]; s_l[j] = l[nt]; }
+#pragma unroll
+            for (int c = 0; c < MT; ++c)
+                *reinterpret_cast<float2*>(s_o + j * D + 16 * c + 2 * g) = make_float2((o[nt][c][0] + o[nt][c][1]) * down, (o[nt][c][2] + o[nt][c][3]) * down);
+        }
+    }
+};
+
+// s8: products on mma m16n8k32, the codes as they are; the other operand in fixed point, 23 bits of its largest value, as three digits that take
+// three of four columns, so that the eight columns are two heads.  Sums are exact: integers, up to where a reference changes.
+//   q        s8 digits (balanced: -128 .. 127), sum of c_i 256^i
+//   P.V      w = 2^22 e^(s + ln scale - M) with a reference M of its own that follows the largest of these products (so neither a small scale nor a small
+//            probability costs digits that the result needs), as u8 digits.  M and the probabilities' reference m may be left behind by a factor of 4:
+//            w < 2^24.  Sums of 1024 units stay below 2^31 (32 x 127 x 255 each); then, and when a reference follows, they go over into fp32.
+// A lane holds the score of head 2 nt + t / 2 at position g + 8 (t % 2) of each tile.
+template <int D, int NT, bool GIVEN>
+struct EngineS8 {
+    static constexpr int H = 2 * NT, KS = D / 32, MT = D / 16;
+    using S = Stage<D, H, GIVEN>;
+    uint32_t qf[GIVEN ? 1 : NT][KS][2];
+    float q_scale[NT], m[NT], l[NT], big[NT];                    // big: M; all of head 2 nt + t / 2
+    int acc[NT][MT][4];
+    float o[NT][MT];                                              // column 16 c + 2g + t % 2 of that head, over e^M / 2^22
+    int held;                                                     // units in acc
+
+    __device__ __forceinline__ void start(const uint8_t* q_s) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        held = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt] = big[nt] = -INFINITY;
+            l[nt] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                o[nt][mt] = 0.f;
+                acc[nt][mt][0] = acc[nt][mt][1] = acc[nt][mt][2] = acc[nt][mt][3] = 0;
+            }
+        }
+        if constexpr (!GIVEN) {   // columns 0, 1, 2: head 0's digits, most significant first; 4, 5, 6: head 1's
+            const float* scale = reinterpret_cast<const float*>(q_s + H * 4 * D);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int w = 0; w < 2 * KS; ++w)
+                    qf[nt][w >> 1][w & 1] = *reinterpret_cast<const uint32_t*>(q_s + ((nt * 2 + (g >> 2)) * 4 + (g & 3)) * D + k_column<D>(w, t));
+                q_scale[nt] = scale[nt * 2 + (t >> 1)];
+            }
+        }
+    }
+
+    // The queries' digits [H][4][D] (the fourth is 0) and their scales [H]: a head to a warp
+    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh) {
+        const int lane = threadIdx.x & 31;
+        for (int j = threadIdx.x >> 5; j < H; j += kAttendWarps) {
+            float x[D / 32];
+            const float amax = query_of<D>(x, p, b, h0 + j, j < nh);
+            const int ex = exponent(amax);
+            const float up = pow2(min(21 - ex, 127));
+            uint8_t* q = q_s + j * 4 * D + lane * (D / 32);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) {
+                int v = __float2int_rn(x[e] * up);                                   // |v| <= 2^22
+                const int lo = (int)(int8_t)v;
+                v = (v - lo) >> 8;
+                const int mid = (int)(int8_t)v;
+                q[e] = (uint8_t)((v - mid) >> 8); q[D + e] = (uint8_t)mid; q[2 * D + e] = (uint8_t)lo; q[3 * D + e] = 0;
+            }
+            // (a query that is not finite has no digits: its scores are NaN)
+            if (lane == 0) reinterpret_cast<float*>(q_s + H * 4 * D)[j] = amax < INFINITY ? pow2(max(ex - 21, -126)) * rsqrtf((float)D) : __uint_as_float(0x7fc00000u);
+        }
+    }
+
+    // The sums so far go over into o, whose unit then changes by `f`
+    __device__ __forceinline__ void flush(const float* f) {
+        const bool odd = threadIdx.x & 1;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                int* a = acc[nt][mt];
+                o[nt][mt] = (o[nt][mt] + digits_sum(a, odd)) * f[nt];
+                a[0] = a[1] = a[2] = a[3] = 0;
+            }
+        held = 0;
+    }
+
+    // Digits are columns 4i, 4i + 1 (even lanes) and 4i + 2 (odd ones): an even lane ends up with row g's sum, an odd one with row g + 8's
+    static __device__ __forceinline__ float digits_sum(const int* a, bool odd) {
+        const float x = odd ? (float)a[0] : fmaf((float)a[0], 65536.f, (float)a[1] * 256.f);
+        const float y = odd ? (float)a[2] : fmaf((float)a[2], 65536.f, (float)a[3] * 256.f);
+        return (odd ? y : x) + __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+    }
+
+    __device__ __forceinline__ void unit(const AttendParams& p, const uint8_t* st, int pos0, int L, int b, int h0, int nh) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const bool odd = t & 1;
+        const int at = g + 8 * (t & 1);
+        float s[kUnit][NT], lv[kUnit], vs[kUnit];
+        bool grown = false;
+#pragma unroll
+        for (int u = 0; u < kUnit; ++u) {
+            const float2 sc = reinterpret_cast<const float2*>(st + S::kScales)[u];
+            vs[u] = sc.y;
+            lv[u] = __log2f(sc.y);
+            const int pos = pos0 + u * kPageBlock + at;
+            const bool on = reinterpret_cast<const int*>(st + S::kThere)[u] && pos < L;
+            if constexpr (!GIVEN) {
+                int c[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0;
+                uint32_t kw[2][2 * KS];
+                load_k<D>(kw, st, u);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        mma_s8<true>(c[nt], kw[0][2 * ks], kw[1][2 * ks], kw[0][2 * ks + 1], kw[1][2 * ks + 1], qf[nt][ks][0], qf[nt][ks][1]);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[u][nt] = digits_sum(c[nt], odd) * (sc.x * q_scale[nt]);
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int h = nt * 2 + (t >> 1);
+                    s[u][nt] = h < nh ? reinterpret_cast<const float*>(st)[h * kUnitRows + u * kPageBlock + at] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int h = nt * 2 + (t >> 1);
+                if (!GIVEN && p.out_scores && on && h < nh) put_row(p, b, h0 + h, pos, s[u][nt]);
+                s[u][nt] = on ? s[u][nt] * kLog2e : -INFINITY;
+                grown |= s[u][nt] > m[nt] + 2.f || s[u][nt] + lv[u] > big[nt] + 1.99f;
+            }
+        }
+        if (__any_sync(0xffffffffu, grown) || held == 1024) {
+            float f[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float mx = m[nt], bg = big[nt];
+#pragma unroll
+                for (int u = 0; u < kUnit; ++u) { mx = fmaxf(mx, s[u][nt]); bg = fmaxf(bg, s[u][nt] + lv[u]); }
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    if (off == 2) continue;               // (lanes t / 2 = 0 and 1 have different heads)
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                    bg = fmaxf(bg, __shfl_xor_sync(0xffffffffu, bg, off));
+                }
+                l[nt] *= mx == -INFINITY ? 1.f : exp2_(m[nt] - mx);
+                f[nt] = bg == -INFINITY ? 1.f : exp2_(big[nt] - bg);
+                m[nt] = mx;
+                big[nt] = bg;
+            }
+            flush(f);
+        }
+        ++held;
+        uint32_t bf[NT][kUnit];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float ref = m[nt] == -INFINITY ? 0.f : m[nt], w_ref = big[nt] == -INFINITY ? 0.f : big[nt];
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) {
+                l[nt] += fmaf(vs[u], 0.f, exp2_(s[u][nt] - ref));            // (a scale that is NaN reaches the output through the sum)
+                const uint32_t w = __float2uint_rn(exp2_(s[u][nt] + lv[u] - w_ref) * 4194304.f);
+                // rows of the two matrices: positions g and g + 8; an even lane has the two leading digits, an odd one the last
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, w, 1), pick = odd ? 0x4440 : 0x4142;
+                const uint32_t d0 = transpose8x8(__byte_perm(odd ? other : w, 0u, pick)), d1 = transpose8x8(__byte_perm(odd ? w : other, 0u, pick));
+                bf[nt][u] = __byte_perm(d0, d1, 0x6420);  // column g's digits at positions 2t, 2t + 1, 2t + 8, 2t + 9
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < MT; c += 2) {
+            uint32_t v[kUnit][4];
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) load_v<D>(v[u], st + S::kV, u, c);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t a0 = __byte_perm(v[0][2 * x], v[0][2 * x + 1], 0x6420), a1 = __byte_perm(v[0][2 * x], v[0][2 * x + 1], 0x7531);
+                const uint32_t a2 = __byte_perm(v[1][2 * x], v[1][2 * x + 1], 0x6420), a3 = __byte_perm(v[1][2 * x], v[1][2 * x + 1], 0x7531);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_s8<false>(acc[nt][c + x], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void finish(float* s_m, float* s_l, float* s_o) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        float f[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) f[nt] = big[nt] == -INFINITY ? 0.f : exp2_(big[nt] - m[nt]) * (1.f / 4194304.f);
+        flush(f);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1)
+                if (off != 2) l[nt] += __shfl_xor_sync(0xffffffffu, l[nt], off);
+            const int j = nt * 2 + (t >> 1);
+            if (g == 0 && !(t & 1)) { s_m[j] = m[nt]; s_l[j] = l[nt]; }
+#pragma unroll
+            for (int c = 0; c < MT; ++c) s_o[j * D + 16 * c + 2 * g + (t & 1)] = o[nt][c];
+        }
+    }
+};
+
 template <int FMT, int D, int NT, bool GIVEN>
-__global__ void __launch_bounds__(kAttendThreads, Stage<D, 4 * NT, GIVEN>::kCtas) paged_attend_kernel(const __grid_constant__ AttendParams p) {
-    constexpr int KW = D / 16, MT = D / 16;               // words of a lane per K row; tiles of 16 output columns
-    constexpr int H = 4 * NT, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
+using Engine = std::conditional_t<FMT == LISA_S8, EngineS8<D, NT, GIVEN>, EngineF16<D, NT, GIVEN>>;
+
+template <int FMT, int D, int NT, bool GIVEN>
+__global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN>::kCtas) paged_attend_kernel(const __grid_constant__ AttendParams p) {
+    constexpr int H = Engine<FMT, D, NT, GIVEN>::H, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
     using S = Stage<D, H, GIVEN>;
     extern __shared__ __align__(128) uint8_t smem[];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int b = blockIdx.z, split = blockIdx.x, kvh = blockIdx.y / p.passes, pass = blockIdx.y % p.passes;
     const int h0 = kvh * p.G + pass * p.heads, nh = min(p.heads, p.G - pass * p.heads);
     const PagedView& pool = p.pool;
@@ -151,171 +583,17 @@ __global__ void __launch_bounds__(kAttendThreads, Stage<D, 4 * NT, GIVEN>::kCtas
 #pragma unroll
     for (int i = 0; i < S::kCount - 1; ++i) ask(i, i);
 
-    // q as B fragments: column g is head g / 2's leading (even g) or second term
-    uint32_t qf[NT][KW][2];
-    float q_scale[NT];                                    // of the head whose scores this lane gets: head t
+    Engine<FMT, D, NT, GIVEN> engine;
     if constexpr (!GIVEN) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int j = nt * 4 + (g >> 1);
-            float x[KW][4], amax = 0.f;
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const int d0 = D == 128 ? (w >> 2) * 64 + 16 * t + 4 * (w & 3) : 4 * KW * t + 4 * w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[w][e] = j < nh ? ld_elem(p.q.ptr, b * p.q.sb + (h0 + j) * p.q.sh + d0 + e, p.q.dtype) : 0.f;
-                    amax = fmaxf(amax, fabsf(x[w][e]));
-                }
-            }
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            const int ex = exponent(amax);
-            const float up = pow2(13 - ex);
-#pragma unroll
-            for (int w = 0; w < KW; ++w)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    qf[nt][w][e] = pack16(term_of(x[w][2 * e] * up, g & 1), term_of(x[w][2 * e + 1] * up, g & 1));
-            q_scale[nt] = pow2(__shfl_sync(0xffffffffu, ex, 8 * t) - 13) * rsqrtf((float)D);
-        }
+        Engine<FMT, D, NT, GIVEN>::prepare(p, smem + S::kQuery, b, h0, nh);
+        __syncthreads();
     }
-
-    float m[NT], l[NT], o[NT][MT][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = -INFINITY;
-        l[nt] = 0.f;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[nt][mt][e] = 0.f;
-    }
-    int r_exp = kLeastExp;                                // V enters as code * 2^13 scale / 2^r_exp
-
+    engine.start(smem + S::kQuery);
     for (int i = 0, stage = 0; i < mine; ++i, stage = stage + 1 == S::kCount ? 0 : stage + 1) {
         cp_wait<S::kCount - 2>();
         __syncwarp();                                     // unit i is there, and every lane has done with unit i - 1
         ask(i + S::kCount - 1, stage == 0 ? S::kCount - 1 : stage - 1);
-        const uint8_t* st = ring + stage * S::kBytes;
-        const int pos0 = tile_of(i * kUnit) * kPageBlock + g;
-        float s[kUnit][NT][2], vs[kUnit];
-        bool there[kUnit];
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u) {
-            const float2 sc = reinterpret_cast<const float2*>(st + S::kScales)[u];
-            vs[u] = sc.y;
-            there[u] = reinterpret_cast<const int*>(st + S::kThere)[u];
-            if constexpr (!GIVEN) {
-                float c[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
-                uint32_t kw[2][KW];
-                constexpr int W = KW < 4 ? KW : 4;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int row = u * kPageBlock + g + 8 * e;
-#pragma unroll
-                    for (int x = 0; x < KW / W; ++x)
-                        lds_words<W>(&kw[e][x * W], st + row * D + (D == 128 ? k_chunk<D>(row, 4 * x + t) * 16 : 4 * KW * t));
-                }
-#pragma unroll
-                for (int w = 0; w < KW; ++w) {
-                    const uint32_t x0 = biased<FMT>(kw[0][w]), x1 = biased<FMT>(kw[1][w]);
-                    const uint32_t a0 = pair16<FMT>(x0, false), a1 = pair16<FMT>(x1, false), a2 = pair16<FMT>(x0, true), a3 = pair16<FMT>(x1, true);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(c[nt], a0, a1, a2, a3, qf[nt][w][0], qf[nt][w][1]);
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float f = sc.x * q_scale[nt];
-                    s[u][nt][0] = (c[nt][0] + c[nt][1]) * f;
-                    s[u][nt][1] = (c[nt][2] + c[nt][3]) * f;
-                }
-            } else {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int h = nt * 4 + t;
-                        s[u][nt][e] = h < nh ? reinterpret_cast<const float*>(st)[h * kUnitRows + u * kPageBlock + g + 8 * e] : 0.f;
-                    }
-            }
-        }
-        // running maximum
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float mx = m[nt];
-#pragma unroll
-            for (int u = 0; u < kUnit; ++u)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int pos = pos0 + u * kPageBlock + 8 * e;
-                    const bool on = there[u] && pos < L;
-                    if (!GIVEN && p.out_scores && on && nt * 4 + t < nh) {
-                        const int64_t to = b * p.sc_sb + (h0 + nt * 4 + t) * p.sc_sh + pos;
-                        if (p.row_bf16) st_row<true>(p.out_scores, to, s[u][nt][e]);
-                        else st_row<false>(p.out_scores, to, s[u][nt][e]);
-                    }
-                    if (!on) s[u][nt][e] = -INFINITY;
-                    mx = fmaxf(mx, s[u][nt][e]);
-                }
-#pragma unroll
-            for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            if (__any_sync(0xffffffffu, mx > m[nt])) {
-                const float f = mx == -INFINITY ? 1.f : __expf(m[nt] - mx);
-                l[nt] *= f;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
-                m[nt] = mx;
-            }
-        }
-        // V's scales enter with the probabilities; their common power of two follows the largest so far
-        int ex = r_exp;
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u) ex = max(ex, exponent(vs[u]));
-        if (ex > r_exp) {
-            const float f = pow2(max(r_exp - ex, -126));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
-            r_exp = ex;
-        }
-        const float up = pow2(min(13 - r_exp, 127));
-#pragma unroll
-        for (int u = 0; u < kUnit; ++u) {
-            uint32_t bf[NT][2];
-            const float f = vs[u] * up;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float ref = m[nt] == -INFINITY ? 0.f : m[nt];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float pj = __expf(s[u][nt][e] - ref);
-                    l[nt] += pj;
-                    bf[nt][e] = transpose8x8(two_terms(pj * f));
-                }
-            }
-            // ldmatrix.trans on pairs of bytes: a lane gets the columns 16 c + 2g, + 1 of positions 2t, 2t + 1 (and 8 further on), rows g and g + 8 of tile c
-            const int l_row = u * kPageBlock + (lane & 15), l_c = lane >> 4;       // the row this lane addresses, and its chunk of the two in a load
-#pragma unroll
-            for (int c = 0; c < MT; c += 2) {
-                uint32_t v[4];
-                ldmatrix_trans(v, st + S::kV + l_row * D + v_chunk<D>(l_row, c + l_c) * 16);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const uint32_t y0 = biased<FMT>(v[2 * x]), y1 = biased<FMT>(v[2 * x + 1]);
-                    const uint32_t a0 = across16<FMT>(y0, false), a1 = across16<FMT>(y0, true), a2 = across16<FMT>(y1, false), a3 = across16<FMT>(y1, true);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + x], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
-                }
-            }
-        }
+        engine.unit(p, ring + stage * S::kBytes, tile_of(i * kUnit) * kPageBlock, L, b, h0, nh);
     }
 
     // warps joined, in the memory of the rings
@@ -324,17 +602,7 @@ __global__ void __launch_bounds__(kAttendThreads, Stage<D, 4 * NT, GIVEN>::kCtas
     float* s_o = reinterpret_cast<float*>(smem);          // [warps][H][D]
     float* s_m = s_o + kAttendWarps * H * D;              // [warps][H]
     float* s_l = s_m + kAttendWarps * H;
-    const float down = pow2(max(r_exp - 13, -126));
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) l[nt] += __shfl_xor_sync(0xffffffffu, l[nt], off);
-        const int j = warp * H + nt * 4 + t;
-        if (g == 0) { s_m[j] = m[nt]; s_l[j] = l[nt]; }
-#pragma unroll
-        for (int c = 0; c < MT; ++c)
-            *reinterpret_cast<float2*>(s_o + j * D + 16 * c + 2 * g) = make_float2((o[nt][c][0] + o[nt][c][1]) * down, (o[nt][c][2] + o[nt][c][3]) * down);
-    }
+    engine.finish(s_m + warp * H, s_l + warp * H, s_o + warp * H * D);
     __syncthreads();
     for (int e = tid; e < nh * (D / 4); e += kAttendThreads) {
         const int j = e / (D / 4), x = e % (D / 4) * 4;
@@ -346,7 +614,7 @@ __global__ void __launch_bounds__(kAttendThreads, Stage<D, 4 * NT, GIVEN>::kCtas
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kAttendWarps; ++w) {
-            const float f = __expf(s_m[w * H + j] - ref);
+            const float f = exp2_(s_m[w * H + j] - ref);
             const float4 v = *reinterpret_cast<const float4*>(s_o + (w * H + j) * D + x);
             den = fmaf(f, s_l[w * H + j], den);
             acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
@@ -379,7 +647,7 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
 #pragma unroll 4
     for (int c = 0; c < parts; ++c) {
         const size_t part = base + (size_t)c * p.Hq;
-        const float f = __expf(p.ws_m[part] - ref);
+        const float f = exp2_(p.ws_m[part] - ref);
         den = fmaf(f, p.ws_l[part], den);
         acc = fmaf(f, p.ws_o[part * d + threadIdx.x], acc);
     }
@@ -390,8 +658,8 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant_
 constexpr int kMinTiles = kUnit * kAttendWarps;           // of a CTA: less would leave warps without work
 constexpr int kSplitCtas = 8;                             // CTAs an SM is given at most by splitting
 
-int column_tiles(int G) { return G > 4 ? 2 : 1; }
-int head_passes(int G) { return (G + 4 * column_tiles(G) - 1) / (4 * column_tiles(G)); }
+// Query heads that a CTA takes: two (s8) or four (e4m3) to a column tile, one or two (s8: four) of those
+int heads_per_cta(int dtype, int G) { return dtype == LISA_S8 ? (G > 4 ? 8 : G > 2 ? 4 : 2) : G > 4 ? 8 : 4; }
 
 // CTAs a sequence is split over: what per_sm CTAs an SM take in whole waves, counted in tiles, each CTA with the cost of its start and end, and the merge.
 int splits_for(int64_t ctas, int tiles, int per_sm, bool given) {
@@ -406,21 +674,31 @@ int splits_for(int64_t ctas, int tiles, int per_sm, bool given) {
     return (int)best;
 }
 
-// Room for the parts of a step: splitting makes no more than kSplitCtas CTAs an SM, of 4 or 8 heads each, and none below kMinTiles tiles.
+// Room for the parts of a step: splitting makes no more than kSplitCtas CTAs an SM, of up to 8 heads each, and none below kMinTiles tiles.
 size_t part_bytes(int B, int Hq, int Hkv, int d, int L) {
     const int64_t tiles = (L + kPageBlock - 1) / kPageBlock;
-    const int64_t most = kSplitCtas * (int64_t)sm_count() * 4 * column_tiles(Hq / Hkv), all = (int64_t)B * Hq * ((tiles + kMinTiles - 1) / kMinTiles);
+    const int64_t most = kSplitCtas * (int64_t)sm_count() * std::min(Hq / Hkv, 8), all = (int64_t)B * Hq * ((tiles + kMinTiles - 1) / kMinTiles);
     const size_t n = ((size_t)std::min(most, all) + 3) & ~(size_t)3;
     return (n * (2 + (size_t)d) * sizeof(float) + 255) & ~(size_t)255;
 }
 
+template <int FMT, int D, int NT, bool GIVEN>
+struct Attend {
+    using S = Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN>;
+    static cudaError_t launch(const AttendParams& p, cudaStream_t s) {
+        void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, NT, GIVEN>;
+        const cudaError_t e = allow_smem(kernel, S::kTotal, true);
+        return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.splits, p.pool.Hkv * p.passes, p.B), dim3(kAttendThreads), S::kTotal, s, p);
+    }
+};
+
 template <int FMT, bool GIVEN>
 cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
-    const int nt = column_tiles(p.G), all_tiles = (p.L + kPageBlock - 1) / kPageBlock;
-    p.heads = 4 * nt;
-    p.passes = head_passes(p.G);
+    const int all_tiles = (p.L + kPageBlock - 1) / kPageBlock;
+    p.heads = heads_per_cta(FMT, p.G);
+    p.passes = (p.G + p.heads - 1) / p.heads;
     const int64_t ctas = (int64_t)p.B * p.pool.Hkv * p.passes;
-    const int splits = splits_for(ctas, all_tiles, nt == 2 ? Stage<128, 8, GIVEN>::kCtas : Stage<128, 4, GIVEN>::kCtas, GIVEN);
+    const int splits = splits_for(ctas, all_tiles, p.heads == 8 ? Stage<128, 8, GIVEN>::kCtas : Stage<128, 4, GIVEN>::kCtas, GIVEN);
     p.tiles = ((all_tiles + splits - 1) / splits + kMinTiles - 1) / kMinTiles * kMinTiles;
     p.splits = (all_tiles + p.tiles - 1) / p.tiles;
     const size_t n = ((size_t)p.B * p.splits * p.Hq + 3) & ~(size_t)3;     // (not used where nothing is split)
@@ -428,11 +706,10 @@ cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
     p.ws_l = p.ws_m + n;
     p.ws_o = p.ws_l + n;
     auto attend = [&](auto width) -> cudaError_t {
-        constexpr int D = decltype(width)::value;
-        void (*kernel)(AttendParams) = nt == 2 ? paged_attend_kernel<FMT, D, 2, GIVEN> : paged_attend_kernel<FMT, D, 1, GIVEN>;
-        const size_t smem = nt == 2 ? Stage<D, 8, GIVEN>::kTotal : Stage<D, 4, GIVEN>::kTotal;
-        const cudaError_t e = allow_smem(kernel, smem, true);
-        return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.splits, p.pool.Hkv * p.passes, p.B), dim3(kAttendThreads), smem, s, p);
+        constexpr int D = decltype(width)::value, per = FMT == LISA_S8 ? 2 : 4;
+        if constexpr (FMT == LISA_S8)
+            if (p.heads == 2) return Attend<FMT, D, 1, GIVEN>::launch(p, s);
+        return p.heads == 4 ? Attend<FMT, D, 4 / per, GIVEN>::launch(p, s) : Attend<FMT, D, 8 / per, GIVEN>::launch(p, s);
     };
     cudaError_t e = p.pool.d == 128 ? attend(std::integral_constant<int, 128>{}) : p.pool.d == 64 ? attend(std::integral_constant<int, 64>{})
                                                                                                     : attend(std::integral_constant<int, 32>{});
