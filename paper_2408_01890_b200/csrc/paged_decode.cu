@@ -393,13 +393,6 @@ struct EngineS8 {
         held = 0;
     }
 
-    // Digits are columns 4i, 4i + 1 (even lanes) and 4i + 2 (odd ones): an even lane ends up with row g's sum, an odd one with row g + 8's
-    static __device__ __forceinline__ float digits_sum(const int* a, bool odd) {
-        const float x = odd ? (float)a[0] : fmaf((float)a[0], 65536.f, (float)a[1] * 256.f);
-        const float y = odd ? (float)a[2] : fmaf((float)a[2], 65536.f, (float)a[3] * 256.f);
-        return (odd ? y : x) + __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
-    }
-
     __device__ __forceinline__ void unit(const AttendParams& p, const uint8_t* st, int pos0, int L, int b, int h0, int nh) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         const bool odd = t & 1;

@@ -23,6 +23,13 @@ __device__ __forceinline__ void mma_s8(int* d, uint32_t a0, uint32_t a1, uint32_
         asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// A product whose second operand are base-256 digits in columns 4i, 4i + 1 (lanes with even t) and 4i + 2 (odd t): an even lane ends up with row g's
+// sum, an odd one with row g + 8's
+__device__ __forceinline__ float digits_sum(const int* c, bool odd) {
+    const float x = odd ? (float)c[0] : fmaf((float)c[0], 65536.f, (float)c[1] * 256.f);
+    const float y = odd ? (float)c[2] : fmaf((float)c[2], 65536.f, (float)c[3] * 256.f);
+    return (odd ? y : x) + __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+}
 // fp16 mma with k = 8
 __device__ __forceinline__ void mma_f16_k8(float* d, uint32_t a0, uint32_t a1, uint32_t b0) {
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"

@@ -2,12 +2,12 @@
 //
 //   a = W2^T act(W1^T prev + b1) + b2 + q'.K'_j / sqrt(r)     (Eq. 3-4; and the other forms of Integrate)
 //
-// A CTA takes CH positions of a sequence and all heads, because the aligner mixes them.  Phase 1: the differences of all heads into shared memory, a
-// warp per KV head.  K' lies with the 16 positions of a block side by side, so 16 bytes are one rank at 16 positions: on mma m16n8k16 the
-// rows of tile mt are positions 2 mt and 2 mt + 1 of the eight blocks, k are the ranks (up to 32, zeros beyond r), the columns the two fp16 terms of q'
-// for four query heads.  Phase 2: the FFN, a warp to 16 positions (M), on mma m16n8k16 with every fp32 operand as three bf16 terms (24 bits) against the
-// bf16 weights, whose products are exact: rows handed on in fp32 are what fp32 arithmetic gives.  A row that is bf16 is one term.
-// With fewer than 128 positions to a CTA (small batches) the hidden units are divided over the warps and their sums added in a fixed order.
+// A CTA takes chunks of CH positions of a sequence and all heads, because the aligner mixes them.  Phase 1: the differences of all heads into shared
+// memory, a warp per KV head, whose K' come by cp.async into a ring of the warp's own.  K' lies with the 16 positions of a block side by side, so
+// transposing loads of pairs of bytes give the A operand of a product over ranks, positions being its rows; the columns are digits (s8) or terms
+// (e4m3) of q', as in paged_decode.cu.  Phase 2: the FFN, a warp to 16 positions (M), on mma m16n8k16 with every fp32 operand as three bf16 terms (24 bits)
+// against the bf16 weights, whose products are exact: rows handed on in fp32 are what fp32 arithmetic gives.  A row that is bf16 is one term.
+// With fewer than 16 positions to a warp (small batches) the hidden units are divided over the warps and their sums added in a fixed order.
 // Bytes: r of K' a KV head and position, the row in and out; bound by HBM for large batches, else by the latency of its two phases.
 #include <algorithm>
 
@@ -106,7 +106,7 @@ size_t general_smem(const ScoresParams& p) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kRingHeads = 3;            // KV heads' K' of a warp on their way or in use
 
-// Shared memory of a CTA (byte offsets): differences [HQ][CH + 4], partial FFN outputs [HS][HQ][CH + 4] (HS > 1), the two terms of q' [HQ][2][32] and its
+// Shared memory of a CTA (byte offsets): differences [HQ][CH + 4], partial FFN outputs [HS][HQ][CH + 4] (HS > 1), q' as operands (128 bytes a head) and its
 // scales, weights, biases, and the warps' rings: a stage is [CH / 16 blocks][24 or 32 ranks][16 positions] and the blocks' scales
 struct ScoresLayout {
     int y, qp, q_scale, w1, w2, b1, b2, ring, stage, scales, total;
@@ -116,7 +116,7 @@ __host__ __device__ inline ScoresLayout scores_layout(int HQ, int NW, int CH, bo
     const int HS = NW * 16 / CH, mp = (m + 15) / 16 * 16, kp = concat ? 2 * HQ : (HQ + 15) / 16 * 16;
     int off = HQ * (CH + 4) * 4;
     l.y = off; off += HS > 1 ? HS * HQ * (CH + 4) * 4 : 0;
-    l.qp = off; off += HQ * 2 * kMaxRank * 2;
+    l.qp = off; off += HQ * 128;
     l.q_scale = off; off += HQ * 4;
     l.w1 = off; off += kp * (mp + 8) * 2;
     l.w2 = off; off += mp * (HQ + 8) * 2;
@@ -129,42 +129,107 @@ __host__ __device__ inline ScoresLayout scores_layout(int HQ, int NW, int CH, bo
     return l;
 }
 
-// Differences of up to four query heads of one KV head, whose K' lies in a stage: positions 2g and 2g + 1 of a block are rows g and g + 8, ranks are k
+// Differences of a KV head's G query heads, whose K' lies in a stage: a block's positions 2g and 2g + 1 are rows g and g + 8 of A, ranks are k.  q: the
+// heads' operands; s_s: their rows of differences.
+//   e4m3  codes as fp16, q' as two fp16 terms [2][32]: column g is head g / 2's leading (even g) or second term
+//   s8    codes as they are, q' as three s8 digits [4][32] (the fourth is 0, ranks in the order that A has them): columns 4i .. 4i + 2 are head i's
 template <int FMT, int NB>
-__device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, bool wide, const __half* q, const float* q_scale, int nh, float* s_s, int ld) {
+__device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, bool wide, const uint8_t* q, const float* q_scale, int G, float* s_s, int ld) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, ranks = wide ? 32 : 24;
-    // column g: head g / 2's leading (even g) or second term
-    uint32_t bf[4];
-    const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (g >> 1) * 2 * kMaxRank + (g & 1) * kMaxRank) + t;
+    const float2* sc = reinterpret_cast<const float2*>(stage + scales);
+    if constexpr (FMT == LISA_S8) {
+        uint32_t a[NB][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bf[i] = (g >> 1) < nh && (wide || i < 3) ? qr[4 * i] : 0u;
-    const float qs = t < nh ? q_scale[t] : 0.f;
+        for (int k = 0; k < NB; ++k) {   // (what a block of 24 ranks has behind them meets digits of 0)
+            uint32_t w[4];
+            ldmatrix_trans(w, stage + (k * ranks + lane) * 16);
+            a[k][0] = __byte_perm(w[0], w[1], 0x6420); a[k][1] = __byte_perm(w[0], w[1], 0x7531);
+            a[k][2] = __byte_perm(w[2], w[3], 0x6420); a[k][3] = __byte_perm(w[2], w[3], 0x7531);
+        }
+        for (int h0 = 0; h0 < G; h0 += 2) {
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 2)) * 128 + (g & 3) * 32) + t;
+            const bool has = h0 + (g >> 2) < G, mine = h0 + (t >> 1) < G;
+            const uint32_t b0 = has ? qr[0] : 0u, b1 = has ? qr[4] : 0u;
+            const float qs = mine ? q_scale[h0 + (t >> 1)] : 0.f;
+            float* to = s_s + (h0 + (t >> 1)) * ld + 2 * g + (t & 1);
 #pragma unroll
-    for (int k = 0; k < NB; ++k) {
-        uint32_t w[4];
-        ldmatrix_trans(w, stage + (k * ranks + lane) * 16);
-        float c[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < NB; ++k) {
+                int c[4] = {0, 0, 0, 0};
+                mma_s8<true>(c, a[k][0], a[k][1], a[k][2], a[k][3], b0, b1);
+                const float x = digits_sum(c, t & 1) * (sc[k].x * qs);
+                if (mine) to[k * kPageBlock] = x;
+            }
+        }
+    } else {
+        for (int h0 = 0; h0 < G; h0 += 4) {
+            uint32_t bf[4];
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 1)) * 128 + (g & 1) * 64) + t;
+            const bool has = h0 + (g >> 1) < G, mine = h0 + t < G;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = biased<FMT>(w[i]);
-        mma_f16(c, across16<FMT>(w[0], false), across16<FMT>(w[0], true), across16<FMT>(w[1], false), across16<FMT>(w[1], true), bf[0], bf[1]);
-        if (wide) mma_f16(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), across16<FMT>(w[3], false), across16<FMT>(w[3], true), bf[2], bf[3]);
-        else mma_f16_k8(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), bf[2]);
-        const float f = reinterpret_cast<const float2*>(stage + scales)[k].x * qs;
-        if (t < nh) *reinterpret_cast<float2*>(s_s + t * ld + k * kPageBlock + 2 * g) = make_float2((c[0] + c[1]) * f, (c[2] + c[3]) * f);
+            for (int i = 0; i < 4; ++i) bf[i] = has && (wide || i < 3) ? qr[4 * i] : 0u;
+            const float qs = mine ? q_scale[h0 + t] : 0.f;
+#pragma unroll
+            for (int k = 0; k < NB; ++k) {
+                uint32_t w[4];
+                ldmatrix_trans(w, stage + (k * ranks + lane) * 16);
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(c, across16<FMT>(w[0], false), across16<FMT>(w[0], true), across16<FMT>(w[1], false), across16<FMT>(w[1], true), bf[0], bf[1]);
+                if (wide) mma_f16(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), across16<FMT>(w[3], false), across16<FMT>(w[3], true), bf[2], bf[3]);
+                else mma_f16_k8(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), bf[2]);
+                const float f = sc[k].x * qs;
+                if (mine) *reinterpret_cast<float2*>(s_s + (h0 + t) * ld + k * kPageBlock + 2 * g) = make_float2((c[0] + c[1]) * f, (c[2] + c[3]) * f);
+            }
+        }
     }
 }
 
-template <int HQ, int NW, int CH, bool CONCAT>
-__global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(const __grid_constant__ ScoresParams p, int dtype) {
+// q' of N heads as operands: lane = rank
+template <int FMT, int N>
+__device__ __forceinline__ void query_operands(const ScoresParams& p, int b, int first, int step, int HQ, uint8_t* qp_s, float* q_scale) {
+    const int lane = threadIdx.x & 31, r = p.pool.r;
+    float x[N];                           // all loads in flight together
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int h = first + i * step;
+        x[i] = lane < r && h < HQ ? ld_elem(p.qp.ptr, b * p.qp.sb + h * p.qp.sh + lane, p.qp.dtype) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int h = first + i * step;
+        if (h >= HQ) break;
+        const float amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x[i]) & 0x7fffffffu));
+        const int ex = exponent(amax);
+        if constexpr (FMT == LISA_S8) {
+            int v = __float2int_rn(x[i] * pow2(min(21 - ex, 127)));          // |v| <= 2^22
+            const int lo = (int)(int8_t)v;
+            v = (v - lo) >> 8;
+            const int mid = (int)(int8_t)v;
+            uint8_t* at = qp_s + h * 128 + (lane & 16) + (lane >> 1 & 3) * 4 + (lane >> 3 & 1) * 2 + (lane & 1);
+            at[0] = (uint8_t)((v - mid) >> 8); at[32] = (uint8_t)mid; at[64] = (uint8_t)lo; at[96] = 0;
+            if (lane == 0) q_scale[h] = amax < INFINITY ? pow2(max(ex - 21, -126)) * rsqrtf((float)r) : __uint_as_float(0x7fc00000u);
+        } else {
+            const float y = x[i] * pow2(13 - ex);
+            __half* at = reinterpret_cast<__half*>(qp_s + h * 128) + lane;
+            const __half hi = __float2half_rn(y);
+            at[0] = hi;
+            at[32] = __float2half_rn(y - __half2float(hi));
+            if (lane == 0) q_scale[h] = pow2(ex - 13) * rsqrtf((float)r);
+        }
+    }
+}
+
+// A CTA takes `per` chunks of CH positions one after the other: its weights and q' serve them all, and K' of the next is asked for while the FFN runs.
+template <int FMT, int HQ, int NW, int CH, bool CONCAT>
+__global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(const __grid_constant__ ScoresParams p, int per) {
     constexpr int THREADS = NW * 32, HS = NW * 16 / CH, LD = CH + 4, NB = CH / kPageBlock, NT2 = HQ / 8, KPH = (HQ + 15) / 16;
     constexpr int KS1 = CONCAT ? 2 * HQ / 16 : KPH, W2_LD = HQ + 8;
     extern __shared__ __align__(16) uint8_t smem_b[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int b = blockIdx.y, j0 = blockIdx.x * CH, m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8, r = p.pool.r;
+    const int b = blockIdx.y, m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8, r = p.pool.r;
     const ScoresLayout lay = scores_layout(HQ, NW, CH, CONCAT, m, r);
     float* s_s = reinterpret_cast<float*>(smem_b);
     float* y_s = reinterpret_cast<float*>(smem_b + lay.y);
-    __half* qp_s = reinterpret_cast<__half*>(smem_b + lay.qp);
+    uint8_t* qp_s = smem_b + lay.qp;
     float* q_scale = reinterpret_cast<float*>(smem_b + lay.q_scale);
     __nv_bfloat16* w1_s = reinterpret_cast<__nv_bfloat16*>(smem_b + lay.w1);     // [inputs][mp + 8], zero rows and columns beyond the FFN's sizes
     __nv_bfloat16* w2_s = reinterpret_cast<__nv_bfloat16*>(smem_b + lay.w2);     // [mp][HQ + 8]
@@ -189,192 +254,224 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     for (int e = lane; e < kRingHeads * lay.stage / 16; e += 32) reinterpret_cast<uint4*>(ring)[e] = make_uint4(0u, 0u, 0u, 0u);   // ranks beyond r stay zero
     __syncwarp();
     chain_wait();
-    const int L = length_of(p.seq_lens, b, p.L);
-    if (j0 >= L) {
+    const int L = length_of(p.seq_lens, b, p.L), first = blockIdx.x * per, chunks = min(per, (L + CH - 1) / CH - first);
+    if (chunks <= 0) {
         cp_wait<0>();
         return;
     }
 
-    // lane i: page of the chunk's block i
-    const int id = lane < NB && j0 + lane * kPageBlock < L ? p.pool.page_of(b, j0 + lane * kPageBlock, warp == 0) : -1;
-    const uint32_t there = __ballot_sync(0xffffffffu, id >= 0);
-    const uint8_t* kp_at[NB];             // this lane's rank of KV head 0 in each block
-#pragma unroll
-    for (int k = 0; k < NB; ++k)
-        kp_at[k] = p.pool.page(max(__shfl_sync(0xffffffffu, id, k), 0)) + p.pool.kp_block(0, j0 + k * kPageBlock) + lane * kPageBlock;
-    const uint8_t* scale_at = reinterpret_cast<const uint8_t*>(p.pool.scales(p.pool.page(max(id, 0)), 0, j0 + lane * kPageBlock));
-    const int blocks = 1 << (p.pool.shift - 4), passes = (p.G + 3) / 4, n_kv = p.pool.Hkv;
+    // lane i: page of block i of a chunk
+    auto id_of = [&](int chunk) {
+        const int pos = (first + chunk) * CH + lane * kPageBlock;
+        return chunk < chunks && lane < NB && pos < L ? p.pool.page_of(b, pos, warp == 0) : -1;
+    };
+    const int blocks = 1 << (p.pool.shift - 4), n_kv = p.pool.Hkv, heads = n_kv > warp ? (n_kv - warp + NW - 1) / NW : 0;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-    auto ask = [&](int kvh, int stage) {
-        if (kvh < n_kv) {
+    // what is being asked for: the chunk's blocks (this lane's rank of KV head 0), the head; and the pages of the chunk behind it
+    const uint8_t *kp_at[NB], *scale_at;
+    uint32_t there_ask;
+    int ask_chunk = 0, ask_head = 0, id_next;
+    auto enter = [&](int id, int chunk) {
+        const int j0 = (first + chunk) * CH;
+        there_ask = __ballot_sync(0xffffffffu, id >= 0);
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+            kp_at[k] = p.pool.page(max(__shfl_sync(0xffffffffu, id, k), 0)) + p.pool.kp_block(0, j0 + k * kPageBlock) + lane * kPageBlock;
+        scale_at = reinterpret_cast<const uint8_t*>(p.pool.scales(p.pool.page(max(id, 0)), 0, j0 + (lane < NB ? lane : 0) * kPageBlock));
+        id_next = id_of(chunk + 1);
+    };
+    auto ask = [&](int stage) {
+        if (ask_chunk < chunks && heads > 0) {
             const uint32_t to = ring_at + stage * lay.stage;
-            const int64_t head = (int64_t)kvh * blocks;
+            const int64_t head = (int64_t)(warp + ask_head * NW) * blocks;
 #pragma unroll
             for (int k = 0; k < NB; ++k)
-                if (lane < r) cp_async<16>(to + (k * (r > 24 ? 32 : 24) + lane) * 16, kp_at[k] + head * (r * kPageBlock), there >> k & 1);
-            if (lane < NB) cp_async<8>(to + lay.scales + lane * 8, scale_at + head * 8, id >= 0);
+                if (lane < r) cp_async<16>(to + (k * (r > 24 ? 32 : 24) + lane) * 16, kp_at[k] + head * (r * kPageBlock), there_ask >> k & 1);
+            if (lane < NB) cp_async<8>(to + lay.scales + lane * 8, scale_at + head * 8, there_ask >> lane & 1);
+            if (++ask_head == heads) {
+                ask_head = 0;
+                if (++ask_chunk < chunks) enter(id_next, ask_chunk);
+            }
         }
         cp_commit();
     };
+    int id = id_of(0);
+    enter(id, 0);
+    uint32_t there = there_ask;           // blocks of the chunk being worked on whose page is there
 #pragma unroll
-    for (int i = 0; i < kRingHeads - 1; ++i) ask(warp + i * NW, i);
+    for (int i = 0; i < kRingHeads - 1; ++i) ask(i);
+    query_operands<FMT, (HQ + NW - 1) / NW>(p, b, warp, NW, HQ, qp_s, q_scale);
+    __syncthreads();
 
-    // the previous scores of the FFN phase: asked for now
     const int strip = warp % NB, hs = warp / NB, p0 = strip * 16 + g, p1 = p0 + 8;
-    const bool ok0 = j0 + p0 < L, ok1 = j0 + p1 < L;
-    float pv[KPH * 4][2];               // slots 2 i, 2 i + 1: heads 8 i + 2t, + 1
-    auto load_prev = [&](const auto* row) {
-        row += b * p.prev_sb + j0 + 2 * t * p.prev_sh;
+    int stage = 0;
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int j0 = (first + chunk) * CH;
+        const bool ok0 = j0 + p0 < L, ok1 = j0 + p1 < L;
+        // the previous scores of the FFN phase: asked for now
+        float pv[KPH * 4][2];             // slots 2 i, 2 i + 1: heads 8 i + 2t, + 1
+        auto load_prev = [&](const auto* row) {
+            row += b * p.prev_sb + j0 + 2 * t * p.prev_sh;
 #pragma unroll
-        for (int i = 0; i < KPH * 2; ++i) {
-            const bool in = i < HQ / 8;
+            for (int i = 0; i < KPH * 2; ++i) {
+                const bool in = i < HQ / 8;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const auto* at = row + (8 * i + e) * p.prev_sh;
-                pv[2 * i + e][0] = in && ok0 ? (float)at[p0] : 0.f;
-                pv[2 * i + e][1] = in && ok1 ? (float)at[p1] : 0.f;
-            }
-        }
-    };
-    if (p.row_bf16) load_prev(static_cast<const __nv_bfloat16*>(p.prev));
-    else load_prev(static_cast<const float*>(p.prev));
-
-    // q', each head brought to [2^13, 2^14) by a power of two, as two fp16 terms
-    for (int h = warp; h < HQ; h += NW) {
-        float x = lane < r ? ld_elem(p.qp.ptr, b * p.qp.sb + h * p.qp.sh + lane, p.qp.dtype) : 0.f;
-        const int ex = exponent(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu)));
-        x *= pow2(13 - ex);
-        const __half hi = __float2half_rn(x);
-        qp_s[h * 2 * kMaxRank + lane] = hi;
-        qp_s[h * 2 * kMaxRank + kMaxRank + lane] = __float2half_rn(x - __half2float(hi));
-        if (lane == 0) q_scale[h] = pow2(ex - 13) * rsqrtf((float)r);
-    }
-    __syncthreads();
-
-    // phase 1
-    for (int kvh = warp, stage = 0; kvh < n_kv; kvh += NW, stage = stage + 1 == kRingHeads ? 0 : stage + 1) {
-        cp_wait<kRingHeads - 2>();
-        __syncwarp();
-        ask(kvh + (kRingHeads - 1) * NW, stage == 0 ? kRingHeads - 1 : stage - 1);
-        for (int pass = 0; pass < passes; ++pass) {
-            const int h0 = kvh * p.G + pass * 4, nh = min(4, p.G - pass * 4);
-            if (dtype == LISA_S8) delta_blocks<LISA_S8, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + h0 * 2 * kMaxRank, q_scale + h0, nh, s_s + h0 * LD, LD);
-            else delta_blocks<LISA_E4M3, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + h0 * 2 * kMaxRank, q_scale + h0, nh, s_s + h0 * LD, LD);
-        }
-    }
-    cp_wait<0>();                         // (the weights; a warp without heads has not waited)
-    __syncthreads();
-
-    // the FFN: a warp owns 16 positions and every HS-th block of 16 hidden units
-    float yacc[NT2][4];
-#pragma unroll
-    for (int j = 0; j < NT2; ++j) {
-        const float x = hs == 0 ? b2_s[j * 8 + 2 * t] : 0.f, y = hs == 0 ? b2_s[j * 8 + 2 * t + 1] : 0.f;
-        yacc[j][0] = x; yacc[j][1] = y; yacc[j][2] = x; yacc[j][3] = y;
-    }
-    uint32_t afr[KS1][3][4];
-#pragma unroll
-    for (int ks = 0; ks < KS1; ++ks)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {   // operand register q: rows g (+ 8), inputs 2t, 2t + 1 (+ 8)
-            const int k8 = ks * 16 + (q & 2 ? 8 : 0);
-            float x, y;
-            if (k8 < KPH * 16 && !(CONCAT && k8 >= HQ)) {
-                x = pv[k8 / 4][q & 1]; y = pv[k8 / 4 + 1][q & 1];
-            } else {
-                const float* d = s_s + (k8 - HQ + 2 * t) * LD + (q & 1 ? p1 : p0);
-                x = d[0]; y = d[LD];
-            }
-            split3(x, y, afr[ks][0][q], afr[ks][1][q], afr[ks][2][q]);
-        }
-    const bool one_term = p.row_bf16 && !CONCAT;      // (a bf16 row is its own first term)
-    const int lk = (lane & 7) + (lane & 8 ? 8 : 0), ln = lane & 16 ? 8 : 0;   // row and column half this lane addresses for ldmatrix
-    for (int blk = hs; blk < mp / 16; blk += HS) {
-        float hacc[2][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            hacc[u][0] = hacc[u][2] = b1_s[blk * 16 + u * 8 + 2 * t];
-            hacc[u][1] = hacc[u][3] = b1_s[blk * 16 + u * 8 + 2 * t + 1];
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS1; ++ks) {
-            uint32_t w[4];
-            ldsm_x4_trans(w, w1_s + (ks * 16 + lk) * w1_ld + blk * 16 + ln);
-            if (!one_term) {
-#pragma unroll
-                for (int q = 2; q >= 1; --q) {        // smallest terms first
-                    mma_bf16(hacc[0], afr[ks][q], w[0], w[1]);
-                    mma_bf16(hacc[1], afr[ks][q], w[2], w[3]);
+                for (int e = 0; e < 2; ++e) {
+                    const auto* at = row + (8 * i + e) * p.prev_sh;
+                    pv[2 * i + e][0] = in && ok0 ? (float)at[p0] : 0.f;
+                    pv[2 * i + e][1] = in && ok1 ? (float)at[p1] : 0.f;
                 }
             }
-            mma_bf16(hacc[0], afr[ks][0], w[0], w[1]);
-            mma_bf16(hacc[1], afr[ks][0], w[2], w[3]);
+        };
+        if (p.row_bf16) load_prev(static_cast<const __nv_bfloat16*>(p.prev));
+        else load_prev(static_cast<const float*>(p.prev));
+
+        // phase 1
+        for (int i = 0; i < heads; ++i) {
+            const int kvh = warp + i * NW;
+            cp_wait<kRingHeads - 2>();
+            __syncwarp();
+            ask(stage == 0 ? kRingHeads - 1 : stage - 1);
+            delta_blocks<FMT, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + kvh * p.G * 128, q_scale + kvh * p.G, p.G, s_s + kvh * p.G * LD, LD);
+            stage = stage + 1 == kRingHeads ? 0 : stage + 1;
         }
-        uint32_t hfr[3][4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                split3(act_apply(hacc[u][2 * e], p.act), act_apply(hacc[u][2 * e + 1], p.act), hfr[0][2 * u + e], hfr[1][2 * u + e], hfr[2][2 * u + e]);
-#pragma unroll
-        for (int j = 0; j < NT2; j += 2) {
-            uint32_t w[4];
-            const __nv_bfloat16* src = w2_s + (blk * 16 + lk) * W2_LD + j * 8;
-            if (j + 1 < NT2) ldsm_x4_trans(w, src + ln);
-            else ldsm_x2_trans(w, src);
-#pragma unroll
-            for (int q = 2; q >= 0; --q) {
-                mma_bf16(yacc[j], hfr[q], w[0], w[1]);
-                if (j + 1 < NT2) mma_bf16(yacc[j + 1], hfr[q], w[2], w[3]);
-            }
-        }
-    }
-    // yacc[j]: [0] (p0, head 8 j + 2t), [1] (p0, + 1), [2] (p1, 2t), [3] (p1, + 1)
-    if constexpr (HS == 1) {
-        if (!(there >> strip & 1)) return;
-        const bool also = p.out_scores;
-        float* to = p.scores + b * p.s_sb + 2 * t * p.s_sh + j0;
-#pragma unroll
-        for (int j = 0; j < NT2; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int h = j * 8 + (e & 1), pos = e & 2 ? p1 : p0;
-                const float v = yacc[j][e] + (CONCAT ? 0.f : s_s[(h + 2 * t) * LD + pos]);
-                if (!(e & 2 ? ok1 : ok0)) continue;
-                if (also) put_score(p, b, h + 2 * t, j0 + pos, v);
-                else to[h * p.s_sh + pos] = v;
-            }
-    } else {
-#pragma unroll
-        for (int j = 0; j < NT2; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y_s[(hs * HQ + j * 8 + 2 * t + (e & 1)) * LD + (e & 2 ? p1 : p0)] = yacc[j][e];
+        if (chunk == 0 && heads == 0) cp_wait<0>();      // (the weights)
         __syncthreads();
-        for (int e = tid; e < HQ * CH; e += THREADS) {
-            const int h = e / CH, pos = e % CH;
-            if (j0 + pos >= L || !(there >> (pos / kPageBlock) & 1)) continue;
-            float x = CONCAT ? 0.f : s_s[h * LD + pos];
+
+        // the FFN: a warp owns 16 positions and every HS-th block of 16 hidden units
+        float yacc[NT2][4];
 #pragma unroll
-            for (int q = 0; q < HS; ++q) x += y_s[(q * HQ + h) * LD + pos];
-            put_score(p, b, h, j0 + pos, x);
+        for (int j = 0; j < NT2; ++j) {
+            const float x = hs == 0 ? b2_s[j * 8 + 2 * t] : 0.f, y = hs == 0 ? b2_s[j * 8 + 2 * t + 1] : 0.f;
+            yacc[j][0] = x; yacc[j][1] = y; yacc[j][2] = x; yacc[j][3] = y;
         }
+        uint32_t afr[KS1][3][4];
+#pragma unroll
+        for (int ks = 0; ks < KS1; ++ks)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {   // operand register q: rows g (+ 8), inputs 2t, 2t + 1 (+ 8)
+                const int k8 = ks * 16 + (q & 2 ? 8 : 0);
+                float x, y;
+                if (k8 < KPH * 16 && !(CONCAT && k8 >= HQ)) {
+                    x = pv[k8 / 4][q & 1]; y = pv[k8 / 4 + 1][q & 1];
+                } else {
+                    const float* d = s_s + (k8 - HQ + 2 * t) * LD + (q & 1 ? p1 : p0);
+                    x = d[0]; y = d[LD];
+                }
+                split3(x, y, afr[ks][0][q], afr[ks][1][q], afr[ks][2][q]);
+            }
+        const bool one_term = p.row_bf16 && !CONCAT;      // (a bf16 row is its own first term)
+        const int lk = (lane & 7) + (lane & 8 ? 8 : 0), ln = lane & 16 ? 8 : 0;   // row and column half this lane addresses for ldmatrix
+        for (int blk = hs; blk < mp / 16; blk += HS) {
+            float hacc[2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                hacc[u][0] = hacc[u][2] = b1_s[blk * 16 + u * 8 + 2 * t];
+                hacc[u][1] = hacc[u][3] = b1_s[blk * 16 + u * 8 + 2 * t + 1];
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS1; ++ks) {
+                uint32_t w[4];
+                ldsm_x4_trans(w, w1_s + (ks * 16 + lk) * w1_ld + blk * 16 + ln);
+                if (!one_term) {
+#pragma unroll
+                    for (int q = 2; q >= 1; --q) {        // smallest terms first
+                        mma_bf16(hacc[0], afr[ks][q], w[0], w[1]);
+                        mma_bf16(hacc[1], afr[ks][q], w[2], w[3]);
+                    }
+                }
+                mma_bf16(hacc[0], afr[ks][0], w[0], w[1]);
+                mma_bf16(hacc[1], afr[ks][0], w[2], w[3]);
+            }
+            uint32_t hfr[3][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    split3(act_apply(hacc[u][2 * e], p.act), act_apply(hacc[u][2 * e + 1], p.act), hfr[0][2 * u + e], hfr[1][2 * u + e], hfr[2][2 * u + e]);
+#pragma unroll
+            for (int j = 0; j < NT2; j += 2) {
+                uint32_t w[4];
+                const __nv_bfloat16* src = w2_s + (blk * 16 + lk) * W2_LD + j * 8;
+                if (j + 1 < NT2) ldsm_x4_trans(w, src + ln);
+                else ldsm_x2_trans(w, src);
+#pragma unroll
+                for (int q = 2; q >= 0; --q) {
+                    mma_bf16(yacc[j], hfr[q], w[0], w[1]);
+                    if (j + 1 < NT2) mma_bf16(yacc[j + 1], hfr[q], w[2], w[3]);
+                }
+            }
+        }
+        // yacc[j]: [0] (p0, head 8 j + 2t), [1] (p0, + 1), [2] (p1, 2t), [3] (p1, + 1)
+        if constexpr (HS == 1) {
+            if (there >> strip & 1) {
+                const bool also = p.out_scores;
+                float* to = p.scores + b * p.s_sb + 2 * t * p.s_sh + j0;
+#pragma unroll
+                for (int j = 0; j < NT2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int h = j * 8 + (e & 1), pos = e & 2 ? p1 : p0;
+                        const float v = yacc[j][e] + (CONCAT ? 0.f : s_s[(h + 2 * t) * LD + pos]);
+                        if (!(e & 2 ? ok1 : ok0)) continue;
+                        if (also) put_score(p, b, h + 2 * t, j0 + pos, v);
+                        else to[h * p.s_sh + pos] = v;
+                    }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NT2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y_s[(hs * HQ + j * 8 + 2 * t + (e & 1)) * LD + (e & 2 ? p1 : p0)] = yacc[j][e];
+            __syncthreads();
+            for (int e = tid; e < HQ * CH; e += THREADS) {
+                const int h = e / CH, pos = e % CH;
+                if (j0 + pos >= L || !(there >> (pos / kPageBlock) & 1)) continue;
+                float x = CONCAT ? 0.f : s_s[h * LD + pos];
+#pragma unroll
+                for (int q = 0; q < HS; ++q) x += y_s[(q * HQ + h) * LD + pos];
+                put_score(p, b, h, j0 + pos, x);
+            }
+        }
+        if (chunk + 1 == chunks) break;
+        __syncthreads();                  // the differences give way to the next chunk's
+        id = id_of(chunk + 1);
+        there = __ballot_sync(0xffffffffu, id >= 0);
     }
+    cp_wait<0>();
 }
 
-template <int HQ, bool CONCAT>
-cudaError_t launch_fast(const ScoresParams& p, int dtype, cudaStream_t s) {
+template <int FMT, int HQ, bool CONCAT>
+cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
     // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128.  Fewer positions where that
     // does not give every SM two CTAs.
     constexpr int NW = CONCAT ? 8 : 4;
     int ch = NW * 16;
     while (ch > 16 && (int64_t)p.B * ((p.L + ch - 1) / ch) < 2 * (int64_t)sm_count()) ch /= 2;
-    void (*kernel)(ScoresParams, int) = ch == 64 ? paged_scores_kernel<HQ, NW, 64, CONCAT> : ch == 32 ? paged_scores_kernel<HQ, NW, 32, CONCAT>
-                                                                                          : paged_scores_kernel<HQ, NW, 16, CONCAT>;
+    void (*kernel)(ScoresParams, int) = ch == 64 ? paged_scores_kernel<FMT, HQ, NW, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, NW, 32, CONCAT>
+                                                                                               : paged_scores_kernel<FMT, HQ, NW, 16, CONCAT>;
     if constexpr (CONCAT)
-        if (ch == 128) kernel = paged_scores_kernel<HQ, NW, 128, CONCAT>;
+        if (ch == 128) kernel = paged_scores_kernel<FMT, HQ, NW, 128, CONCAT>;
     const size_t smem = (size_t)scores_layout(HQ, NW, ch, CONCAT, p.m, p.pool.r).total;
     const cudaError_t e = allow_smem(kernel, smem, true);
-    return e != cudaSuccess ? e : launch_chained(kernel, dim3((p.L + ch - 1) / ch, p.B), dim3(NW * 32), smem, s, p, dtype);
+    if (e != cudaSuccess) return e;
+    // chunks to a CTA: whole waves of as many CTAs as an SM holds, a CTA's start counted as half a chunk
+    const int n = (p.L + ch - 1) / ch;
+    const int64_t slots = (CONCAT ? 2 : 4) * (int64_t)sm_count();
+    int per = 1;
+    int64_t least = INT64_MAX;
+    for (int q = 1; q <= n && q <= 32; ++q) {
+        const int64_t cost = ((int64_t)p.B * ((n + q - 1) / q) + slots - 1) / slots * (2 * q + 1);
+        if (cost < least) { least = cost; per = q; }
+    }
+    return launch_chained(kernel, dim3((n + per - 1) / per, p.B), dim3(NW * 32), smem, s, p, per);
+}
+
+template <int FMT>
+cudaError_t launch_typed(const ScoresParams& p, cudaStream_t s) {
+    const bool concat = p.integrate == LISA_INTEGRATE_CONCAT;
+    if (p.Hq == 40) return concat ? launch_fast<FMT, 40, true>(p, s) : launch_fast<FMT, 40, false>(p, s);
+    return concat ? launch_fast<FMT, 32, true>(p, s) : launch_fast<FMT, 32, false>(p, s);
 }
 
 bool vec16(const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0; }
@@ -386,9 +483,7 @@ cudaError_t launch_paged_scores(const ScoresParams& p, int dtype, cudaStream_t s
                       vec16(p.w1) && vec16(p.w2);
     cudaError_t e;
     if (fast) {
-        const bool concat = p.integrate == LISA_INTEGRATE_CONCAT;
-        if (p.Hq == 40) e = concat ? launch_fast<40, true>(p, dtype, s) : launch_fast<40, false>(p, dtype, s);
-        else e = concat ? launch_fast<32, true>(p, dtype, s) : launch_fast<32, false>(p, dtype, s);
+        e = dtype == LISA_S8 ? launch_typed<LISA_S8>(p, s) : launch_typed<LISA_E4M3>(p, s);
     } else {
         const size_t smem = general_smem(p);
         auto kernel = dtype == LISA_S8 ? paged_scores_general_kernel<LISA_S8> : paged_scores_general_kernel<LISA_E4M3>;
