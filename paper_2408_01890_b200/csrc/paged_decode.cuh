@@ -26,8 +26,8 @@ __device__ __forceinline__ void mma_s8(int* d, uint32_t a0, uint32_t a1, uint32_
 // A product whose second operand are base-256 digits in columns 4i, 4i + 1 (lanes with even t) and 4i + 2 (odd t): an even lane ends up with row g's
 // sum, an odd one with row g + 8's
 __device__ __forceinline__ float digits_sum(const int* c, bool odd) {
-    const float x = odd ? (float)c[0] : fmaf((float)c[0], 65536.f, (float)c[1] * 256.f);
-    const float y = odd ? (float)c[2] : fmaf((float)c[2], 65536.f, (float)c[3] * 256.f);
+    const float f0 = odd ? 1.f : 65536.f, f1 = odd ? 0.f : 256.f;       // (the same for every call: registers)
+    const float x = fmaf((float)c[0], f0, (float)c[1] * f1), y = fmaf((float)c[2], f0, (float)c[3] * f1);
     return (odd ? y : x) + __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
 }
 // fp16 mma with k = 8
@@ -70,13 +70,22 @@ __device__ __forceinline__ int exponent(float x) {
 
 // 16, 8 or 4 bytes from global to shared memory, zeros where !ok (nothing is read then)
 template <int N>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) {
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(ok ? N : 0), "n"(N) : "memory");
+__device__ __forceinline__ void cp_async_bytes(uint32_t dst, const void* src, int bytes) {   // bytes: N or 0
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(N) : "memory");
 }
+template <int N>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) { cp_async_bytes<N>(dst, src, ok ? N : 0); }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The larger of two values, NaN if one is NaN
+__device__ __forceinline__ float max_nan(float x, float y) {
+    float z;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
 
 // A shared layer's scores over the cache (paged_scores.cu)
 struct ScoresParams {

@@ -10,6 +10,7 @@
 // With fewer than 16 positions to a warp (small batches) the hidden units are divided over the warps and their sums added in a fixed order.
 // Bytes: r of K' a KV head and position, the row in and out; bound by HBM for large batches, else by the latency of its two phases.
 #include <algorithm>
+#include <type_traits>
 
 #include "decode_fast.cuh"
 #include "paged_decode.cuh"
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(kGeneralThreads) paged_scores_general_kernel(c
         if (p.ffn_layers == 1) {
             for (int h = 0; h < Hq; ++h) a[h] = hid[h];
         } else {
-            for (int u = 0; u < m; ++u) hid[u] = act_apply(hid[u], p.act);
+            for (int u = 0; u < m; ++u) hid[u] = p.act == LISA_ACT_RELU ? max_nan(hid[u], 0.f) : act_apply(hid[u], p.act);
             for (int h = 0; h < Hq; ++h) {
                 float s = b2_s[h];
                 for (int u = 0; u < m; ++u) s = fmaf(hid[u], w2_s[u * Hq + h], s);
@@ -183,6 +184,12 @@ __device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, b
     }
 }
 
+template <typename T>
+__device__ __forceinline__ T to_row(float x) {
+    if constexpr (sizeof(T) == 2) return __float2bfloat16_rn(x);
+    else return x;
+}
+
 // q' of N heads as operands: lane = rank
 template <int FMT, int N>
 __device__ __forceinline__ void query_operands(const ScoresParams& p, int b, int first, int step, int HQ, uint8_t* qp_s, float* q_scale) {
@@ -267,27 +274,34 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     };
     const int blocks = 1 << (p.pool.shift - 4), n_kv = p.pool.Hkv, heads = n_kv > warp ? (n_kv - warp + NW - 1) / NW : 0;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-    // what is being asked for: the chunk's blocks (this lane's rank of KV head 0), the head; and the pages of the chunk behind it
+    // what is being asked for: this lane's rank of the chunk's blocks and its bytes (0: not there), the head; and the pages of the chunk behind it
+    const uint32_t block_bytes = (r > 24 ? 32 : 24) * 16, head_step = (uint32_t)(NW * blocks * r * kPageBlock), scale_step = (uint32_t)(NW * blocks * 8);
     const uint8_t *kp_at[NB], *scale_at;
-    uint32_t there_ask;
-    int ask_chunk = 0, ask_head = 0, id_next;
+    int kp_bytes[NB], scale_bytes, ask_chunk = 0, ask_head = 0, id_next;
+    uint32_t there_ask, head_at, scale_off;
     auto enter = [&](int id, int chunk) {
         const int j0 = (first + chunk) * CH;
         there_ask = __ballot_sync(0xffffffffu, id >= 0);
 #pragma unroll
-        for (int k = 0; k < NB; ++k)
-            kp_at[k] = p.pool.page(max(__shfl_sync(0xffffffffu, id, k), 0)) + p.pool.kp_block(0, j0 + k * kPageBlock) + lane * kPageBlock;
-        scale_at = reinterpret_cast<const uint8_t*>(p.pool.scales(p.pool.page(max(id, 0)), 0, j0 + (lane < NB ? lane : 0) * kPageBlock));
+        for (int k = 0; k < NB; ++k) {
+            kp_at[k] = p.pool.page(max(__shfl_sync(0xffffffffu, id, k), 0)) + p.pool.kp_block(warp, j0 + k * kPageBlock) + lane * kPageBlock;
+            kp_bytes[k] = there_ask >> k & 1 ? 16 : 0;
+        }
+        scale_at = reinterpret_cast<const uint8_t*>(p.pool.scales(p.pool.page(max(id, 0)), warp, j0 + (lane < NB ? lane : 0) * kPageBlock));
+        scale_bytes = id >= 0 ? 8 : 0;
+        head_at = scale_off = 0;
         id_next = id_of(chunk + 1);
     };
     auto ask = [&](int stage) {
         if (ask_chunk < chunks && heads > 0) {
             const uint32_t to = ring_at + stage * lay.stage;
-            const int64_t head = (int64_t)(warp + ask_head * NW) * blocks;
+            if (lane < r) {
 #pragma unroll
-            for (int k = 0; k < NB; ++k)
-                if (lane < r) cp_async<16>(to + (k * (r > 24 ? 32 : 24) + lane) * 16, kp_at[k] + head * (r * kPageBlock), there_ask >> k & 1);
-            if (lane < NB) cp_async<8>(to + lay.scales + lane * 8, scale_at + head * 8, there_ask >> lane & 1);
+                for (int k = 0; k < NB; ++k) cp_async_bytes<16>(to + lane * 16 + k * block_bytes, kp_at[k] + head_at, kp_bytes[k]);
+            }
+            if (lane < NB) cp_async_bytes<8>(to + lay.scales + lane * 8, scale_at + scale_off, scale_bytes);
+            head_at += head_step;
+            scale_off += scale_step;
             if (++ask_head == heads) {
                 ask_head = 0;
                 if (++ask_chunk < chunks) enter(id_next, ask_chunk);
@@ -311,15 +325,16 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
         // the previous scores of the FFN phase: asked for now
         float pv[KPH * 4][2];             // slots 2 i, 2 i + 1: heads 8 i + 2t, + 1
         auto load_prev = [&](const auto* row) {
-            row += b * p.prev_sb + j0 + 2 * t * p.prev_sh;
+            row += b * p.prev_sb + j0 + 2 * t * p.prev_sh + p0;
+            const int64_t step = p.prev_sh, far = 7 * step;
 #pragma unroll
             for (int i = 0; i < KPH * 2; ++i) {
-                const bool in = i < HQ / 8;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const auto* at = row + (8 * i + e) * p.prev_sh;
-                    pv[2 * i + e][0] = in && ok0 ? (float)at[p0] : 0.f;
-                    pv[2 * i + e][1] = in && ok1 ? (float)at[p1] : 0.f;
+                    const bool in = i < HQ / 8;
+                    pv[2 * i + e][0] = in && ok0 ? (float)row[0] : 0.f;
+                    pv[2 * i + e][1] = in && ok1 ? (float)row[8] : 0.f;
+                    row += e ? far : step;
                 }
             }
         };
@@ -360,6 +375,7 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
                 }
                 split3(x, y, afr[ks][0][q], afr[ks][1][q], afr[ks][2][q]);
             }
+        const float least = p.act == LISA_ACT_RELU ? 0.f : -INFINITY;
         const bool one_term = p.row_bf16 && !CONCAT;      // (a bf16 row is its own first term)
         const int lk = (lane & 7) + (lane & 8 ? 8 : 0), ln = lane & 16 ? 8 : 0;   // row and column half this lane addresses for ldmatrix
         for (int blk = hs; blk < mp / 16; blk += HS) {
@@ -383,12 +399,18 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
                 mma_bf16(hacc[0], afr[ks][0], w[0], w[1]);
                 mma_bf16(hacc[1], afr[ks][0], w[2], w[3]);
             }
+            if (p.act == LISA_ACT_SILU) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { hacc[0][e] = act_apply(hacc[0][e], LISA_ACT_SILU); hacc[1][e] = act_apply(hacc[1][e], LISA_ACT_SILU); }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { hacc[0][e] = max_nan(hacc[0][e], least); hacc[1][e] = max_nan(hacc[1][e], least); }
+            }
             uint32_t hfr[3][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    split3(act_apply(hacc[u][2 * e], p.act), act_apply(hacc[u][2 * e + 1], p.act), hfr[0][2 * u + e], hfr[1][2 * u + e], hfr[2][2 * u + e]);
+                for (int e = 0; e < 2; ++e) split3(hacc[u][2 * e], hacc[u][2 * e + 1], hfr[0][2 * u + e], hfr[1][2 * u + e], hfr[2][2 * u + e]);
 #pragma unroll
             for (int j = 0; j < NT2; j += 2) {
                 uint32_t w[4];
@@ -405,18 +427,26 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
         // yacc[j]: [0] (p0, head 8 j + 2t), [1] (p0, + 1), [2] (p1, 2t), [3] (p1, + 1)
         if constexpr (HS == 1) {
             if (there >> strip & 1) {
-                const bool also = p.out_scores;
-                float* to = p.scores + b * p.s_sb + 2 * t * p.s_sh + j0;
+                auto finish = [&](auto* row, int64_t sb, int64_t sh) {
+                    row += b * sb + 2 * t * sh + j0 + p0;
+                    const float* d = s_s + 2 * t * LD + p0;
+                    const int64_t far = 7 * sh;
 #pragma unroll
-                for (int j = 0; j < NT2; ++j)
+                    for (int j = 0; j < NT2; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int h = j * 8 + (e & 1), pos = e & 2 ? p1 : p0;
-                        const float v = yacc[j][e] + (CONCAT ? 0.f : s_s[(h + 2 * t) * LD + pos]);
-                        if (!(e & 2 ? ok1 : ok0)) continue;
-                        if (also) put_score(p, b, h + 2 * t, j0 + pos, v);
-                        else to[h * p.s_sh + pos] = v;
-                    }
+                        for (int e = 0; e < 2; ++e) {
+                            const int at = (j * 8 + e) * LD;
+                            const float x = yacc[j][e] + (CONCAT ? 0.f : d[at]), y = yacc[j][e + 2] + (CONCAT ? 0.f : d[at + 8]);
+                            if (ok0) row[0] = to_row<std::remove_pointer_t<decltype(row)>>(x);
+                            if (ok1) row[8] = to_row<std::remove_pointer_t<decltype(row)>>(y);
+                            row += e ? far : sh;
+                        }
+                };
+                finish(p.scores, p.s_sb, p.s_sh);
+                if (p.out_scores) {       // (only where it is not where the scores went: a row of bf16)
+                    if (p.row_bf16) finish(static_cast<__nv_bfloat16*>(p.out_scores), p.sc_sb, p.sc_sh);
+                    else finish(static_cast<float*>(p.out_scores), p.sc_sb, p.sc_sh);
+                }
             }
         } else {
 #pragma unroll
