@@ -70,12 +70,12 @@ __device__ __forceinline__ int exponent(float x) {
 
 // 16, 8 or 4 bytes from global to shared memory, zeros where !ok (nothing is read then)
 template <int N>
-__device__ __forceinline__ void cp_async_bytes(uint32_t dst, const void* src, int bytes) {   // bytes: N or 0
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(N) : "memory");
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) {
+    if constexpr (N == 16)
+        asm volatile("{.reg .pred q; setp.eq.b32 q, %2, 0; cp.async.cg.shared.global [%0], [%1], 16, q;}" ::"r"(dst), "l"(src), "r"((int)ok) : "memory");
+    else
+        asm volatile("{.reg .pred q; setp.eq.b32 q, %2, 0; cp.async.ca.shared.global [%0], [%1], %3, q;}" ::"r"(dst), "l"(src), "r"((int)ok), "n"(N) : "memory");
 }
-template <int N>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool ok) { cp_async_bytes<N>(dst, src, ok ? N : 0); }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }

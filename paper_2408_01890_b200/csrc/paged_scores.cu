@@ -147,6 +147,20 @@ __device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, b
             a[k][0] = __byte_perm(w[0], w[1], 0x6420); a[k][1] = __byte_perm(w[0], w[1], 0x7531);
             a[k][2] = __byte_perm(w[2], w[3], 0x6420); a[k][3] = __byte_perm(w[2], w[3], 0x7531);
         }
+        if (NB > 1 && G == 1) {          // one head: its digits take the columns of two, with another block each
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (g & 3) * 32) + t;
+            const uint32_t q0 = qr[0], q1 = qr[4], b0 = g < 4 ? q0 : 0u, b1 = g < 4 ? q1 : 0u, c0 = g < 4 ? 0u : q0, c1 = g < 4 ? 0u : q1;
+            const float qs = q_scale[0];
+            float* to = s_s + (t >> 1) * kPageBlock + 2 * g + (t & 1);
+#pragma unroll
+            for (int k = 0; k < NB; k += 2) {
+                int c[4] = {0, 0, 0, 0};
+                mma_s8<true>(c, a[k][0], a[k][1], a[k][2], a[k][3], b0, b1);
+                mma_s8<true>(c, a[k + 1][0], a[k + 1][1], a[k + 1][2], a[k + 1][3], c0, c1);
+                to[k * kPageBlock] = digits_sum(c, t & 1) * (sc[k + (t >> 1)].x * qs);
+            }
+            return;
+        }
         for (int h0 = 0; h0 < G; h0 += 2) {
             const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 2)) * 128 + (g & 3) * 32) + t;
             const bool has = h0 + (g >> 2) < G, mine = h0 + (t >> 1) < G;
@@ -274,10 +288,11 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     };
     const int blocks = 1 << (p.pool.shift - 4), n_kv = p.pool.Hkv, heads = n_kv > warp ? (n_kv - warp + NW - 1) / NW : 0;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-    // what is being asked for: this lane's rank of the chunk's blocks and its bytes (0: not there), the head; and the pages of the chunk behind it
+    // what is being asked for: this lane's rank of the chunk's blocks and whether they are there, the head; and the pages of the chunk behind it
     const uint32_t block_bytes = (r > 24 ? 32 : 24) * 16, head_step = (uint32_t)(NW * blocks * r * kPageBlock), scale_step = (uint32_t)(NW * blocks * 8);
     const uint8_t *kp_at[NB], *scale_at;
-    int kp_bytes[NB], scale_bytes, ask_chunk = 0, ask_head = 0, id_next;
+    int ask_chunk = 0, ask_head = 0, id_next;
+    bool kp_there[NB], scale_there;
     uint32_t there_ask, head_at, scale_off;
     auto enter = [&](int id, int chunk) {
         const int j0 = (first + chunk) * CH;
@@ -285,10 +300,10 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
             kp_at[k] = p.pool.page(max(__shfl_sync(0xffffffffu, id, k), 0)) + p.pool.kp_block(warp, j0 + k * kPageBlock) + lane * kPageBlock;
-            kp_bytes[k] = there_ask >> k & 1 ? 16 : 0;
+            kp_there[k] = there_ask >> k & 1;
         }
         scale_at = reinterpret_cast<const uint8_t*>(p.pool.scales(p.pool.page(max(id, 0)), warp, j0 + (lane < NB ? lane : 0) * kPageBlock));
-        scale_bytes = id >= 0 ? 8 : 0;
+        scale_there = id >= 0;
         head_at = scale_off = 0;
         id_next = id_of(chunk + 1);
     };
@@ -297,9 +312,9 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
             const uint32_t to = ring_at + stage * lay.stage;
             if (lane < r) {
 #pragma unroll
-                for (int k = 0; k < NB; ++k) cp_async_bytes<16>(to + lane * 16 + k * block_bytes, kp_at[k] + head_at, kp_bytes[k]);
+                for (int k = 0; k < NB; ++k) cp_async<16>(to + lane * 16 + k * block_bytes, kp_at[k] + head_at, kp_there[k]);
             }
-            if (lane < NB) cp_async_bytes<8>(to + lay.scales + lane * 8, scale_at + scale_off, scale_bytes);
+            if (lane < NB) cp_async<8>(to + lay.scales + lane * 8, scale_at + scale_off, scale_there);
             head_at += head_step;
             scale_off += scale_step;
             if (++ask_head == heads) {
