@@ -8,6 +8,7 @@
 // Bound by HBM: 2 bytes in and 1 out per value.
 #include <algorithm>
 
+#include "decode_common.cuh"
 #include "paged_common.cuh"
 
 namespace lisa {
@@ -66,7 +67,7 @@ __device__ __forceinline__ float value_of(const uint32_t* raw, int i) {   // val
     else return __uint_as_float(raw[i]);
 }
 
-// amax as bits, over the warp -> the block's scale, and the factor of what it holds (0: leave it)
+// The block's scale from the largest magnitude of its new values (bits of this lane's) and what it holds
 template <int FMT>
 __device__ __forceinline__ float new_scale(uint32_t amax, float held) {
     const uint32_t all = __reduce_max_sync(0xffffffffu, amax);
@@ -74,55 +75,110 @@ __device__ __forceinline__ float new_scale(uint32_t amax, float held) {
     return all >= 0x7f800000u || !(held == held) ? __uint_as_float(0x7fc00000u) : fmaxf(held, grown);
 }
 
+// Four values as codes by the formula: IEEE division, rounding to nearest even
+template <int FMT>
+__device__ __noinline__ uint32_t encode_exactly(float a, float b, float c, float d, float scale) {
+    return to_code<FMT>(a / scale) | to_code<FMT>(b / scale) << 8 | to_code<FMT>(c / scale) << 16 | to_code<FMT>(d / scale) << 24;
+}
+
+// The same without the division where the reciprocal leaves no doubt: the rounded quotient lies between x lo and x hi, 2^-22 to either side of
+// x / scale, so if both round to the same code that is the code (else, once in some ten thousand values, the division decides).  s8: x lo + 1.5 2^23
+// in one fused multiply-add has the code in its low bits.  With a division for each value 8 x 2048 prompt rows of the 7B shape took 170 us.
+template <int FMT>
+struct Encoder {
+    float scale, lo, hi;
+    bool some, exact;
+    __device__ __forceinline__ explicit Encoder(float s) : scale(s) {
+        const float inv = __frcp_rn(s);
+        lo = inv * (1.f - 0x1p-22f);
+        hi = inv * (1.f + 0x1p-22f);
+        some = s > 0.f;                                   // (false for NaN: codes 0 then)
+        exact = !(s > 0x1p-100f && s < 0x1p100f);         // (a reciprocal out of range, a scale that is not exact to 2^-24)
+    }
+    __device__ __forceinline__ uint32_t operator()(float a, float b, float c, float d) const {
+        uint32_t word, doubt;
+        if constexpr (FMT == LISA_S8) {
+            constexpr float kMagic = 12582912.f;
+            const uint32_t a0 = __float_as_uint(fmaf(a, lo, kMagic)), b0 = __float_as_uint(fmaf(b, lo, kMagic)), c0 = __float_as_uint(fmaf(c, lo, kMagic)),
+                           d0 = __float_as_uint(fmaf(d, lo, kMagic));
+            doubt = (a0 ^ __float_as_uint(fmaf(a, hi, kMagic))) | (b0 ^ __float_as_uint(fmaf(b, hi, kMagic))) | (c0 ^ __float_as_uint(fmaf(c, hi, kMagic))) |
+                    (d0 ^ __float_as_uint(fmaf(d, hi, kMagic)));
+            word = __byte_perm(__byte_perm(a0, b0, 0x0040), __byte_perm(c0, d0, 0x0040), 0x5410);
+        } else {
+            auto pair = [](float x, float y) {            // (the second operand is the low byte)
+                uint16_t v;
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(y), "f"(x));
+                return (uint32_t)v;
+            };
+            word = pair(a * lo, b * lo) | pair(c * lo, d * lo) << 16;
+            doubt = word ^ (pair(a * hi, b * hi) | pair(c * hi, d * hi) << 16);
+        }
+        if (doubt || exact) word = encode_exactly<FMT>(a, b, c, d, scale);
+        return some ? word : 0u;
+    }
+};
+
+// What a block holds, rescaled where its scale has grown
+template <int FMT>
+__device__ __forceinline__ uint32_t rescaled(uint32_t old, float f, bool some) {
+    uint32_t out = 0;
+    if (some)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) out |= to_code<FMT>(__fmul_rn(code_value<FMT>(old, t), f)) << (8 * t);
+    return out;
+}
+
 // D-wide rows (V, and K of a standard layer): 16 bytes per lane and load, all of the block's rows in flight
 template <typename T, int D, int FMT>
 __device__ __forceinline__ void append_rows_block(const RowsParams& p, const TView& src, const Block& x, uint8_t* page) {
     constexpr int VE = 16 / sizeof(T), LR = D / VE, RPI = 32 / LR, NI = kPageBlock / RPI;
     const int lane = threadIdx.x & 31, col = (lane % LR) * VE, r0 = lane / LR;
-    const char* sp = reinterpret_cast<const char*>(src.ptr) + (x.b * src.sb + (int64_t)x.rel0 * src.sn + x.h * src.sh + col) * (int64_t)sizeof(T);
+    const char* sp = reinterpret_cast<const char*>(src.ptr) + (x.b * src.sb + ((int64_t)x.rel0 + r0) * src.sn + x.h * src.sh + col) * (int64_t)sizeof(T);
+    const int64_t step = src.sn * (int64_t)(RPI * sizeof(T));
     uint32_t raw[NI][4];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
+    for (int i = 0; i < NI; ++i, sp += step) {
         const int row = i * RPI + r0;
-        uint4 q = make_uint4(0u, 0u, 0u, 0u);
-        if (row >= x.lo && row < x.hi) q = *reinterpret_cast<const uint4*>(sp + (int64_t)row * src.sn * (int64_t)sizeof(T));
+        const uint4 q = ld_stream16_or_zero(sp, row >= x.lo && row < x.hi);
         raw[i][0] = q.x; raw[i][1] = q.y; raw[i][2] = q.z; raw[i][3] = q.w;
     }
     float* scale_at = p.pool.scales(page, x.h, x.base) + x.is_v;
     const float held = x.lo > 0 ? *scale_at : 0.f;
     uint32_t amax = 0;
+    if constexpr (sizeof(T) == 2) {                       // two at a time, as unsigned halves
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) amax = max(amax, __float_as_uint(value_of<T>(raw[i], e)) & 0x7fffffffu);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t v = raw[i][e] & 0x7fff7fffu;
+                asm("max.u16x2 %0, %0, %1;" : "+r"(amax) : "r"(v));
+            }
+        amax = max(amax << 16, amax & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) amax = max(amax, raw[i][e] & 0x7fffffffu);
+    }
     const float scale = new_scale<FMT>(amax, held);
-    const bool some = scale > 0.f;                      // (false for NaN: codes 0 then)
+    const Encoder<FMT> encode(scale);
     uint8_t* dst = page + (x.is_v ? p.pool.v_off : 0u) + p.pool.row(x.h, x.base) + col;
     if (x.lo > 0 && !(scale == held)) {
         const float f = held / scale;
         for (int e = lane * 4; e < x.lo * D; e += 128) {
             uint32_t* w = reinterpret_cast<uint32_t*>(dst - col + e);
-            const uint32_t old = *w;
-            uint32_t out = 0;
-            if (some)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) out |= to_code<FMT>(code_value<FMT>(old, t) * f) << (8 * t);
-            *w = out;
+            *w = rescaled<FMT>(*w, f, encode.some);
         }
     }
     if (lane == 0) *scale_at = scale;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int row = i * RPI + r0;
-        if (row < x.lo || row >= x.hi) continue;
         uint32_t out[VE / 4];
 #pragma unroll
-        for (int w = 0; w < VE / 4; ++w) {
-            out[w] = 0;
-            if (some)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) out[w] |= to_code<FMT>(value_of<T>(raw[i], 4 * w + t) / scale) << (8 * t);
-        }
+        for (int w = 0; w < VE / 4; ++w)
+            out[w] = encode(value_of<T>(raw[i], 4 * w), value_of<T>(raw[i], 4 * w + 1), value_of<T>(raw[i], 4 * w + 2), value_of<T>(raw[i], 4 * w + 3));
+        if (row < x.lo || row >= x.hi) continue;
         if constexpr (VE == 8) *reinterpret_cast<uint2*>(dst + row * D) = make_uint2(out[0], out[1]);
         else *reinterpret_cast<uint32_t*>(dst + row * D) = out[0];
     }
@@ -136,12 +192,13 @@ __device__ __forceinline__ void append_kp_block(const RowsParams& p, const Block
     const T* sp = reinterpret_cast<const T*>(p.k.ptr) + x.b * p.k.sb + (int64_t)x.rel0 * p.k.sn + x.h * p.k.sh + lane;
     float v[kPageBlock];
 #pragma unroll
-    for (int i = 0; i < kPageBlock; ++i) v[i] = on && i >= x.lo && i < x.hi ? (float)sp[i * p.k.sn] : 0.f;
+    for (int i = 0; i < kPageBlock; ++i, sp += p.k.sn) v[i] = on && i >= x.lo && i < x.hi ? (float)*sp : 0.f;
     uint4* dst = reinterpret_cast<uint4*>(page + p.pool.kp_block(x.h, x.base)) + lane;
     float* scale_at = p.pool.scales(page, x.h, x.base);
     const float held = x.lo > 0 ? *scale_at : 0.f;
+    const bool partial = x.lo > 0 || x.hi < kPageBlock;
     uint32_t old[4] = {0u, 0u, 0u, 0u};
-    if (on && (x.lo > 0 || x.hi < kPageBlock)) {
+    if (on && partial) {
         const uint4 q = *dst;
         old[0] = q.x; old[1] = q.y; old[2] = q.z; old[3] = q.w;
     }
@@ -149,27 +206,28 @@ __device__ __forceinline__ void append_kp_block(const RowsParams& p, const Block
 #pragma unroll
     for (int i = 0; i < kPageBlock; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
     const float scale = new_scale<FMT>(amax, held);
-    const bool some = scale > 0.f, keep = scale == held;
+    const Encoder<FMT> encode(scale);
+    const bool keep = x.lo == 0 || scale == held;
     const float f = held / scale;
     if (lane == 0) *scale_at = scale;
     uint32_t out[4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        out[w] = 0;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int i = 4 * w + t;
-            uint32_t c = (old[w] >> (8 * t)) & 0xffu;
-            if (i >= x.lo && i < x.hi) c = some ? to_code<FMT>(v[i] / scale) : 0u;
-            else if (i < x.lo && !keep) c = some ? to_code<FMT>(code_value<FMT>(old[w], t) * f) : 0u;
-            out[w] |= c << (8 * t);
+        out[w] = encode(v[4 * w], v[4 * w + 1], v[4 * w + 2], v[4 * w + 3]);
+        if (partial) {
+            // bytes of positions before lo (what is held), lo .. hi - 1 (new), and from hi on (as they are)
+            const int lo = min(max(x.lo - 4 * w, 0), 4), hi = min(max(x.hi - 4 * w, 0), 4);
+            const uint32_t below = lo == 4 ? ~0u : (1u << (8 * lo)) - 1u, above = hi == 4 ? 0u : ~0u << (8 * hi);
+            const uint32_t held_w = keep || lo == 0 ? old[w] : rescaled<FMT>(old[w], f, encode.some);
+            out[w] = (out[w] & ~(below | above)) | (held_w & below) | (old[w] & above);
         }
     }
     if (on) *dst = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
+// Four CTAs an SM (two where a block of fp32 rows is in flight): a block is a chain of loads (lengths, table, rows), which other warps have to hide.
 template <typename T, int D, int FMT, bool SHARED>
-__global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 2 : 4) paged_append_kernel(const __grid_constant__ RowsParams p) {
     chain_release();
     chain_wait();
     for (int64_t item = blockIdx.x * (int64_t)kWarps + (threadIdx.x >> 5); item < p.items; item += (int64_t)gridDim.x * kWarps) {
