@@ -178,6 +178,7 @@ lisa_status_t lisa_pages_copy(const lisa_paged_layer* layers, int32_t n_layers, 
     const lisa_status_t st = check_layers(layers, n_layers);
     if (st != LISA_OK) return st;
     if (n < 1 || !src || !dst || !aligned(src, 4) || !aligned(dst, 4)) return LISA_ERR_INVALID_ARG;
+    if ((int64_t)n * n_layers > INT32_MAX) return LISA_ERR_UNSUPPORTED;
     return done(launch_pages_copy(layers, n_layers, src, dst, n, static_cast<cudaStream_t>(stream)));
 }
 

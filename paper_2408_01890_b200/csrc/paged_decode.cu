@@ -49,16 +49,18 @@ constexpr int kUnitRows = kUnit * kPageBlock;
 constexpr int kBatch = 32 / kUnit;                        // units whose pages the lanes hold
 
 // A stage: K rows (or the given scores [heads][32]), V rows, {K's scale, V's scale} of each tile, whether its page is there
-template <int D, int H, bool GIVEN>
+// DEEP: more stages and fewer CTAs to an SM, for grids that leave it at that: a warp then has up to five units on their way.
+template <int D, int H, bool GIVEN, bool DEEP = false>
 struct Stage {
     static constexpr int kFirst = GIVEN ? H * kUnitRows * 4 : kUnitRows * D, kV = kFirst, kScales = kV + kUnitRows * D, kThere = kScales + kUnit * 8;
     static constexpr int kBytes = kThere + 16;
-    static constexpr int kCount = GIVEN ? 3 : 2;
+    static constexpr int kCount = DEEP ? (GIVEN && H <= 4 ? 6 : 5) : GIVEN ? 3 : 2;
     static constexpr int kRing = kBytes * kCount;
     static constexpr int kMerge = kAttendWarps * H * (D + 2) * 4;
     static constexpr int kQuery = (kRing * kAttendWarps > kMerge ? kRing * kAttendWarps : kMerge);     // the queries as operands, behind the rings
     static constexpr int kTotal = kQuery + (GIVEN ? 0 : H * (4 * D + 4));
-    static constexpr int kCtas = H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
+    static constexpr int kCtas = DEEP ? (GIVEN ? 2 : 1) : H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
+    static_assert(kCtas * (kTotal + 1024) <= 227 * 1024 + 1024, "as many CTAs as that fit an SM");
 };
 
 // Rows lie with their 16-byte chunks permuted, so that the eight lanes of a shared-memory access meet eight different ones.  A K access is four
@@ -506,23 +508,24 @@ struct EngineS8 {
 template <int FMT, int D, int NT, bool GIVEN>
 using Engine = std::conditional_t<FMT == LISA_S8, EngineS8<D, NT, GIVEN>, EngineF16<D, NT, GIVEN>>;
 
-template <int FMT, int D, int NT, bool GIVEN>
-__global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN>::kCtas) paged_attend_kernel(const __grid_constant__ AttendParams p) {
+template <int FMT, int D, int NT, bool GIVEN, bool DEEP>
+__global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, DEEP>::kCtas) paged_attend_kernel(const __grid_constant__ AttendParams p) {
     constexpr int H = Engine<FMT, D, NT, GIVEN>::H, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
-    using S = Stage<D, H, GIVEN>;
+    using S = Stage<D, H, GIVEN, DEEP>;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int b = blockIdx.z, split = blockIdx.x, kvh = blockIdx.y / p.passes, pass = blockIdx.y % p.passes;
+    const int kvh = blockIdx.x / p.passes, pass = blockIdx.x % p.passes;
     const int h0 = kvh * p.G + pass * p.heads, nh = min(p.heads, p.G - pass * p.heads);
     const PagedView& pool = p.pool;
     chain_release();
     chain_wait();
-    const int L = length_of(p.seq_lens, b, p.L), all_tiles = (L + kPageBlock - 1) / kPageBlock;
+    int b, split, L;
+    if (!deal_item(p.seq_lens, p.B, p.L, p.tiles * kPageBlock, p.splits, 1, blockIdx.y, b, split, L)) return;
+    const int all_tiles = (L + kPageBlock - 1) / kPageBlock;
     const int first = split * p.tiles, end = min(first + p.tiles, all_tiles), parts = (all_tiles + p.tiles - 1) / p.tiles;
     void* out = const_cast<void*>(p.o.ptr);
-    if (first >= end) {
-        if (L == 0 && split == 0)
-            for (int e = tid; e < nh * D; e += kAttendThreads) st_elem(out, b * p.o.sb + (h0 + e / D) * p.o.sh + e % D, p.o.dtype, 0.f);
+    if (L == 0) {
+        for (int e = tid; e < nh * D; e += kAttendThreads) st_elem(out, b * p.o.sb + (h0 + e / D) * p.o.sh + e % D, p.o.dtype, 0.f);
         return;
     }
 
@@ -530,7 +533,7 @@ __global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GI
     auto tile_of = [&](int k) { return first + (warp + kAttendWarps * (k / kUnit)) * kUnit + k % kUnit; };   // this warp's k-th tile
     auto id_of = [&](int k) {
         const int tile = tile_of(k);
-        return k < mine * kUnit && tile < end ? pool.page_of(b, tile * kPageBlock, blockIdx.y == 0) : -1;
+        return k < mine * kUnit && tile < end ? pool.page_of(b, tile * kPageBlock, blockIdx.x == 0) : -1;
     };
     // lane i: page of tile i of the batch of units that is being asked for; the next batch's are loaded a batch ahead
     int ids = id_of(lane), ids_next = id_of(32 + lane);
@@ -625,46 +628,78 @@ __global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GI
     }
 }
 
-// Joins the parts of a sequence that was split: o = sum_c e^(m_c - M) o_c / sum_c e^(m_c - M) l_c.
-__global__ void __launch_bounds__(128) paged_merge_kernel(const __grid_constant__ AttendParams p) {
-    const int h = blockIdx.x, b = blockIdx.y, d = p.pool.d;
+// Joins the parts of a sequence that was split: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  Bound by latency: the maxima and sums come to a
+// warp's lanes, its partial outputs (four columns a thread, the warps different parts) with them, and one exchange adds the warps' sums.
+constexpr int kMergeThreads = 128;
+__global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(const __grid_constant__ AttendParams p) {
+    constexpr int U = 4;
+    __shared__ float4 s_o[kMergeThreads];
+    const int h = blockIdx.x, b = blockIdx.y, d = p.pool.d, tid = threadIdx.x, lane = tid & 31;
     chain_release();
     chain_wait();
     const int parts = ((length_of(p.seq_lens, b, p.L) + kPageBlock - 1) / kPageBlock + p.tiles - 1) / p.tiles;
-    if (parts <= 1 || threadIdx.x >= d) return;
+    if (parts <= 1) return;
     const size_t base = (size_t)b * p.splits * p.Hq + h;
-    float mx = -INFINITY;
-    for (int c = 0; c < parts; ++c) mx = fmaxf(mx, p.ws_m[base + (size_t)c * p.Hq]);
+    const int lpr = d / 4, x = tid % lpr, c0 = tid / lpr, step = kMergeThreads / lpr;   // lanes of a partial output, this thread's parts
+    const float4* po = reinterpret_cast<const float4*>(p.ws_o + base * d) + x;
+    float4 first[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (c0 + u * step < parts) first[u] = po[(size_t)(c0 + u * step) * p.Hq * lpr];
+    float mx = -INFINITY, den = 0.f;
+    for (int c = lane; c < parts; c += 32) mx = fmaxf(mx, p.ws_m[base + (size_t)c * p.Hq]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     const float ref = mx == -INFINITY ? 0.f : mx;
-    float den = 0.f, acc = 0.f;
+    for (int c = lane; c < parts; c += 32) den = fmaf(exp2_(p.ws_m[base + (size_t)c * p.Hq] - ref), p.ws_l[base + (size_t)c * p.Hq], den);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](int c, const float4& o) {
+        const float w = exp2_(p.ws_m[base + (size_t)c * p.Hq] - ref);
+        acc.x = fmaf(w, o.x, acc.x); acc.y = fmaf(w, o.y, acc.y); acc.z = fmaf(w, o.z, acc.z); acc.w = fmaf(w, o.w, acc.w);
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (c0 + u * step < parts) add(c0 + u * step, first[u]);
 #pragma unroll 4
-    for (int c = 0; c < parts; ++c) {
-        const size_t part = base + (size_t)c * p.Hq;
-        const float f = exp2_(p.ws_m[part] - ref);
-        den = fmaf(f, p.ws_l[part], den);
-        acc = fmaf(f, p.ws_o[part * d + threadIdx.x], acc);
+    for (int c = c0 + U * step; c < parts; c += step) add(c, po[(size_t)c * p.Hq * lpr]);
+    s_o[tid] = acc;
+    __syncthreads();
+    if (tid >= lpr) return;
+    for (int q = 1; q < step; ++q) {
+        const float4 o = s_o[q * lpr + tid];
+        acc.x += o.x; acc.y += o.y; acc.z += o.z; acc.w += o.w;
     }
-    st_elem(const_cast<void*>(p.o.ptr), b * p.o.sb + h * p.o.sh + threadIdx.x, p.o.dtype, den == 0.f ? 0.f : acc / den);
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const int64_t at = b * p.o.sb + h * p.o.sh + 4 * tid;
+    void* out = const_cast<void*>(p.o.ptr);
+    st_elem(out, at, p.o.dtype, acc.x * inv); st_elem(out, at + 1, p.o.dtype, acc.y * inv);
+    st_elem(out, at + 2, p.o.dtype, acc.z * inv); st_elem(out, at + 3, p.o.dtype, acc.w * inv);
 }
 
 // ------------------------------------------------------------------ launches
 constexpr int kMinTiles = kUnit * kAttendWarps;           // of a CTA: less would leave warps without work
-constexpr int kSplitCtas = 8;                             // CTAs an SM is given at most by splitting
+constexpr int kSplitCtas = 16;                            // CTAs an SM is given at most by splitting
 
 // Query heads that a CTA takes: two (s8) or four (e4m3) to a column tile, one or two (s8: four) of those
 int heads_per_cta(int dtype, int G) { return dtype == LISA_S8 ? (G > 4 ? 8 : G > 2 ? 4 : 2) : G > 4 ? 8 : 4; }
 
-// CTAs a sequence is split over: what per_sm CTAs an SM take in whole waves, counted in tiles, each CTA with the cost of its start and end, and the merge.
+// CTAs a sequence is split over: what per_sm CTAs an SM take, counted in tiles, each CTA with the cost of its start and end, and the merge.  Lengths are
+// on the device, where the host cannot read them: equal ones run in whole waves, and of ones spread over [L / 8, L] six tenths are left, whose CTAs fill
+// each other's gaps.  The mean of the two is what is compared, for calls with and without lengths alike, so that both give the same bits.
 int splits_for(int64_t ctas, int tiles, int per_sm, bool given) {
     const int64_t slots = per_sm * (int64_t)sm_count(), most = std::min<int64_t>((tiles + kMinTiles - 1) / kMinTiles, kSplitCtas * (int64_t)sm_count() / ctas);
-    const int64_t start = given ? 16 : 10, merge = given ? 32 : 16;
-    int64_t best = 1, least = INT64_MAX;
-    for (int64_t s = 1; s <= std::max<int64_t>(1, most); ++s) {
+    const double start = given ? 16 : 10, merge = given ? 32 : 16;
+    int best = 1;
+    double least = 1e300;
+    for (int s = 1; s <= std::max<int64_t>(1, most); ++s) {
         const int64_t each = ((tiles + s - 1) / s + kMinTiles - 1) / kMinTiles * kMinTiles;
-        const int64_t cost = (ctas * s + slots - 1) / slots * (each + start) + (s > 1 ? merge : 0);
+        const double waves = 0.5 * ((double)((ctas * s + slots - 1) / slots) + std::max(1., 0.6 * (double)(ctas * s) / (double)slots));
+        const double cost = waves * ((double)each + start) + (s > 1 ? merge : 0);
         if (cost < least) { least = cost; best = s; }
     }
-    return (int)best;
+    return best;
 }
 
 // Room for the parts of a step: splitting makes no more than kSplitCtas CTAs an SM, of up to 8 heads each, and none below kMinTiles tiles.
@@ -677,11 +712,17 @@ size_t part_bytes(int B, int Hq, int Hkv, int d, int L) {
 
 template <int FMT, int D, int NT, bool GIVEN>
 struct Attend {
-    using S = Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN>;
+    template <bool DEEP>
     static cudaError_t launch(const AttendParams& p, cudaStream_t s) {
-        void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, NT, GIVEN>;
+        using S = Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, DEEP>;
+        void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, NT, GIVEN, DEEP>;
         const cudaError_t e = allow_smem(kernel, S::kTotal, true);
-        return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.splits, p.pool.Hkv * p.passes, p.B), dim3(kAttendThreads), S::kTotal, s, p);
+        return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.pool.Hkv * p.passes, p.splits * p.B), dim3(kAttendThreads), S::kTotal, s, p);
+    }
+    // the deep ring where every CTA is resident with it
+    static cudaError_t launch(const AttendParams& p, cudaStream_t s) {
+        const int64_t ctas = (int64_t)p.splits * p.pool.Hkv * p.passes * p.B;
+        return ctas <= (GIVEN ? 2 : 1) * (int64_t)sm_count() ? launch<true>(p, s) : launch<false>(p, s);
     }
 };
 

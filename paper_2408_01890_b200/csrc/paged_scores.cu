@@ -10,6 +10,7 @@
 // With fewer than 16 positions to a warp (small batches) the hidden units are divided over the warps and their sums added in a fixed order.
 // Bytes: r of K' a KV head and position, the row in and out; bound by HBM for large batches, else by the latency of its two phases.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "decode_fast.cuh"
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     constexpr int KS1 = CONCAT ? 2 * HQ / 16 : KPH, W2_LD = HQ + 8;
     extern __shared__ __align__(16) uint8_t smem_b[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int b = blockIdx.y, m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8, r = p.pool.r;
+    const int m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8, r = p.pool.r;
     const ScoresLayout lay = scores_layout(HQ, NW, CH, CONCAT, m, r);
     float* s_s = reinterpret_cast<float*>(smem_b);
     float* y_s = reinterpret_cast<float*>(smem_b + lay.y);
@@ -275,11 +276,12 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     for (int e = lane; e < kRingHeads * lay.stage / 16; e += 32) reinterpret_cast<uint4*>(ring)[e] = make_uint4(0u, 0u, 0u, 0u);   // ranks beyond r stay zero
     __syncwarp();
     chain_wait();
-    const int L = length_of(p.seq_lens, b, p.L), first = blockIdx.x * per, chunks = min(per, (L + CH - 1) / CH - first);
-    if (chunks <= 0) {
+    int b, part, L;
+    if (!deal_item(p.seq_lens, p.B, p.L, per * CH, ((p.L + CH - 1) / CH + per - 1) / per, 0, blockIdx.x, b, part, L)) {
         cp_wait<0>();
         return;
     }
+    const int first = part * per, chunks = min(per, (L + CH - 1) / CH - first);
 
     // lane i: page of block i of a chunk
     auto id_of = [&](int chunk) {
@@ -489,10 +491,13 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
 template <int FMT, int HQ, bool CONCAT>
 cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
     // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128.  Fewer positions where that
-    // does not give every SM two CTAs.
+    // does not give the SMs one and a half.  Eight tenths of the CTAs are taken to have positions (all, where lengths are alike, or six tenths, where they
+    // are spread over [L / 8, L]).
     constexpr int NW = CONCAT ? 8 : 4;
-    int ch = NW * 16;
-    while (ch > 16 && (int64_t)p.B * ((p.L + ch - 1) / ch) < 2 * (int64_t)sm_count()) ch /= 2;
+    constexpr double fill = 0.8;
+    int ch = CONCAT ? 64 : NW * 16;
+    if (CONCAT && fill * p.B * ((p.L + 127) / 128) >= 4 * sm_count()) ch = 128;
+    while (ch > 16 && fill * p.B * ((p.L + ch - 1) / ch) < 1.5 * sm_count()) ch /= 2;
     void (*kernel)(ScoresParams, int) = ch == 64 ? paged_scores_kernel<FMT, HQ, NW, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, NW, 32, CONCAT>
                                                                                                : paged_scores_kernel<FMT, HQ, NW, 16, CONCAT>;
     if constexpr (CONCAT)
@@ -500,16 +505,16 @@ cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
     const size_t smem = (size_t)scores_layout(HQ, NW, ch, CONCAT, p.m, p.pool.r).total;
     const cudaError_t e = allow_smem(kernel, smem, true);
     if (e != cudaSuccess) return e;
-    // chunks to a CTA: whole waves of as many CTAs as an SM holds, a CTA's start counted as half a chunk
+    // chunks to a CTA: whole waves of as many CTAs as an SM holds (of given lengths six tenths, filling each other's gaps), a CTA's start counted as half a chunk
     const int n = (p.L + ch - 1) / ch;
-    const int64_t slots = (CONCAT ? 2 : 4) * (int64_t)sm_count();
+    const double slots = (CONCAT ? 2. : 4.) * sm_count();
     int per = 1;
-    int64_t least = INT64_MAX;
+    double least = 1e300;
     for (int q = 1; q <= n && q <= 32; ++q) {
-        const int64_t cost = ((int64_t)p.B * ((n + q - 1) / q) + slots - 1) / slots * (2 * q + 1);
+        const double x = (double)p.B * ((n + q - 1) / q) / slots, cost = (p.seq_lens ? std::max(1., 0.6 * x) : std::ceil(x)) * (2 * q + 1);
         if (cost < least) { least = cost; per = q; }
     }
-    return launch_chained(kernel, dim3((n + per - 1) / per, p.B), dim3(NW * 32), smem, s, p, per);
+    return launch_chained(kernel, dim3((n + per - 1) / per * p.B), dim3(NW * 32), smem, s, p, per);
 }
 
 template <int FMT>

@@ -5,6 +5,7 @@
 // ascending order and everything that is counted is an integer, so results do not depend on the order of threads.
 #include <algorithm>
 
+#include "decode_common.cuh"
 #include "paged_common.cuh"
 
 namespace lisa {
@@ -14,7 +15,9 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kCopyThreads = 256;
 constexpr int kPiece = 16384;            // bytes that a CTA copies at a time: four 16-byte loads of a thread in flight
+constexpr int kCopyCtas = 8;             // an SM's
 constexpr int kForkCols = 32;
+constexpr int kForkThreads = 512;
 
 struct PagesDev {
     int32_t *table, *lens, *refs;
@@ -40,15 +43,15 @@ PagesDev view_of(const lisa_pages& p) {
 
 // ------------------------------------------------------------------ fork
 // A CTA owns some columns of the table: it has read all of their rows before it writes one, so rows may change places.
-__global__ void __launch_bounds__(256) pages_fork_kernel(const __grid_constant__ PagesDev p, const int32_t* __restrict__ parent) {
+__global__ void __launch_bounds__(kForkThreads) pages_fork_kernel(const __grid_constant__ PagesDev p, const int32_t* __restrict__ parent) {
     extern __shared__ int32_t tile[];    // [B][kForkCols]; in the last CTA the lengths
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     chain_release();
     chain_wait();
     if (blockIdx.x == gridDim.x - 1) {
-        for (int i = tid; i < p.B; i += 256) tile[i] = p.lens[i];
+        for (int i = tid; i < p.B; i += kForkThreads) tile[i] = p.lens[i];
         __syncthreads();
-        for (int i = tid; i < p.B; i += 256) {
+        for (int i = tid; i < p.B; i += kForkThreads) {
             const int from = parent[i];
             const bool ok = (uint32_t)from < (uint32_t)p.B;
             if (!ok && from != -1) atomicAdd(p.status, 1);
@@ -58,10 +61,12 @@ __global__ void __launch_bounds__(256) pages_fork_kernel(const __grid_constant__
     }
     const int c = blockIdx.x * kForkCols + lane;
     const bool in = c < p.max_pages;
-    for (int i = warp; i < p.B; i += 8) tile[i * kForkCols + lane] = in ? p.table[i * p.stride + c] : -1;
+#pragma unroll 4
+    for (int i = warp; i < p.B; i += kForkThreads / 32) tile[i * kForkCols + lane] = in ? p.table[i * p.stride + c] : -1;
     __syncthreads();
     if (!in) return;
-    for (int i = warp; i < p.B; i += 8) {
+#pragma unroll 4
+    for (int i = warp; i < p.B; i += kForkThreads / 32) {
         const int from = parent[i];
         const int old = tile[i * kForkCols + lane], now = (uint32_t)from < (uint32_t)p.B ? tile[from * kForkCols + lane] : -1;
         if (now == old) continue;
@@ -101,11 +106,18 @@ __device__ __forceinline__ int block_scan(int v, int* part, int* total) {
 constexpr int kPer = 4;                  // pages of a thread per round of a scan
 
 __global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __grid_constant__ PagesDev p, const int32_t* __restrict__ n_new) {
-    __shared__ int s_last[kPlanThreads], s_at[kPlanThreads + 1], s_have[kPlanThreads], part[kPlanWarps + 1];
+    __shared__ __align__(16) int s_last[kPlanThreads];
+    __shared__ int s_at[kPlanThreads + 1], s_have[kPlanThreads], part[kPlanWarps + 1];
     __shared__ uint8_t s_copy[kPlanThreads];
     const int tid = threadIdx.x, P = 1 << p.shift;
     chain_release();
     chain_wait();
+    uint32_t free_first = 0;             // free pages among this thread's of the first round
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        const int q = tid * kPer + u;
+        free_first |= (uint32_t)(q < p.n_pages && p.refs[q] == 0) << u;
+    }
     int have = 0, need = 0, last = -1, refs = 0;
     bool bad = false;
     if (tid < p.B) {
@@ -130,7 +142,10 @@ __global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __gri
     // writers of the same page in front of this row; each that copies leaves one entry fewer
     int before = 0;
     if (refs > 1)
-        for (int j = 0; j < tid; ++j) before += s_last[j] == last;
+        for (int j = 0; j < tid; j += 4) {
+            const int4 o = *reinterpret_cast<const int4*>(s_last + j);
+            before += (o.x == last) + (j + 1 < tid && o.y == last) + (j + 2 < tid && o.z == last) + (j + 3 < tid && o.w == last);
+        }
     const bool copy = last >= 0 && refs - before > 1;
     const int wanted = copy + need - have;
     int total, moves, unused;
@@ -142,16 +157,19 @@ __global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __gri
     if (tid == 0) p.head[0] = 0;
     __syncthreads();
     if (total == 0 && !any_bad) return;
-    // are there enough?
-    int free_pages = 0;
-    for (int base = 0; base < p.n_pages && free_pages < total; base += kPlanThreads * kPer) {
-        int mine = 0;
+    // are there enough?  (A thread has kPer neighbouring pages; the first round's were asked for at the start.)
+    auto load_free = [&](int base) {
+        uint32_t bits = 0;
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
-            const int q = base + u * kPlanThreads + tid;
-            mine += q < p.n_pages && p.refs[q] == 0;
+            const int q = base + tid * kPer + u;
+            bits |= (uint32_t)(q < p.n_pages && p.refs[q] == 0) << u;
         }
-        block_scan(mine, part, &unused);
+        return bits;
+    };
+    int free_pages = 0;
+    for (int base = 0; base < p.n_pages && free_pages < total; base += kPlanThreads * kPer) {
+        block_scan(__popc(base ? load_free(base) : free_first), part, &unused);
         free_pages += unused;
     }
     if (any_bad || free_pages < total) {
@@ -164,22 +182,23 @@ __global__ void __launch_bounds__(kPlanThreads) pages_reserve_kernel(const __gri
     if (copy) atomicSub(p.refs + last, 1);
     // the k-th free page goes to the k-th page wanted
     int found = 0;
-    for (int base = 0; base < p.n_pages && found < total; base += kPlanThreads) {
-        const int q = base + tid;
-        const bool free_page = q < p.n_pages && p.refs[q] == 0;
+    for (int base = 0; base < p.n_pages && found < total; base += kPlanThreads * kPer) {
+        uint32_t bits = base ? load_free(base) : free_first;
         int sum;
-        const int k = found + block_scan(free_page, part, &sum);
+        int k = found + block_scan(__popc(bits), part, &sum);
         found += sum;
-        if (!free_page || k >= total) continue;
-        int lo = 0, hi = p.B - 1;        // the last row with s_at <= k: rows that want none share their s_at with the next
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (s_at[mid] <= k) lo = mid; else hi = mid - 1;
+        for (; bits && k < total; bits &= bits - 1, ++k) {
+            const int q = base + tid * kPer + __ffs(bits) - 1;
+            int lo = 0, hi = p.B - 1;    // the last row with s_at <= k: rows that want none share their s_at with the next
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (s_at[mid] <= k) lo = mid; else hi = mid - 1;
+            }
+            const int local = k - s_at[lo];
+            const int slot = s_have[lo] + local - s_copy[lo];   // (a copy's: have - 1)
+            p.table[lo * p.stride + slot] = q;
+            p.refs[q] = 1;
         }
-        const int local = k - s_at[lo];
-        const int slot = s_have[lo] + local - s_copy[lo];   // (a copy's: have - 1)
-        p.table[lo * p.stride + slot] = q;
-        p.refs[q] = 1;
     }
     __syncthreads();
     if (copy) p.dst[move] = p.table[tid * p.stride + have - 1];
@@ -231,7 +250,7 @@ struct CopyParams {
     struct { uint8_t* pages; int64_t bytes; } layer[LISA_MAX_LAYERS];
 };
 
-__global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ CopyParams p) {
+__global__ void __launch_bounds__(kCopyThreads, 4) pages_copy_kernel(const __grid_constant__ CopyParams p) {
     const int tid = threadIdx.x;
     chain_release();
     chain_wait();
@@ -243,26 +262,40 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
         }
     }
     const int n = p.n_dev ? *p.n_dev : p.n;
-    const int64_t items = (int64_t)n * p.n_layers * p.pieces;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int piece = (int)(item % p.pieces), l = (int)(item / p.pieces % p.n_layers), i = (int)(item / p.pieces / p.n_layers);
-        const int64_t bytes = p.layer[l].bytes, at = (int64_t)piece * kPiece;
+    // An item is a page of a layer, or, where there are fewer of those than four to a CTA, a piece of one
+    const int pages = n * p.n_layers, split = pages < 4 * (int)gridDim.x ? p.pieces : 1;      // (below 2^31: the host sees to it)
+    for (int64_t item = blockIdx.x; item < (int64_t)pages * split; item += gridDim.x) {
+        const int page = split == 1 ? (int)item : (int)(item / split), l = page % p.n_layers, i = page / p.n_layers;
+        const int64_t bytes = p.layer[l].bytes;
+        int64_t at = (split == 1 ? 0 : item - (int64_t)page * split) * kPiece;
         if (at >= bytes) continue;
         const int from = p.src[i], into = p.dst[i];
         if (p.status && ((uint32_t)from >= (uint32_t)p.n_pages || (uint32_t)into >= (uint32_t)p.n_pages)) {
-            if (tid == 0 && piece == 0 && l == 0) atomicAdd(p.status, 1);
+            if (tid == 0 && at == 0 && l == 0) atomicAdd(p.status, 1);
             continue;
         }
-        const uint4* s = reinterpret_cast<const uint4*>(p.layer[l].pages + from * bytes + at);
-        uint4* d = reinterpret_cast<uint4*>(p.layer[l].pages + into * bytes + at);
-        const int vecs = (int)min((int64_t)kPiece, bytes - at) / 16;
-        uint4 v[kPiece / 16 / kCopyThreads];
+        const uint8_t* s = p.layer[l].pages + from * bytes + tid * 16;
+        uint8_t* d = p.layer[l].pages + into * bytes + tid * 16;
+        const int64_t end = (split == 1 ? bytes : min(bytes, at + kPiece)) - tid * 16;
+        constexpr int U = kPiece / 16 / kCopyThreads, STEP = 16 * kCopyThreads;
+        uint4 v[U], w[U];
+        auto load = [&](uint4* q, int64_t o) {
 #pragma unroll
-        for (int u = 0; u < kPiece / 16 / kCopyThreads; ++u)
-            if (tid + u * kCopyThreads < vecs) v[u] = s[tid + u * kCopyThreads];
+            for (int u = 0; u < U; ++u)
+                if (o + u * STEP < end) q[u] = ld_stream16(s + o + u * STEP);
+        };
+        auto store = [&](const uint4* q, int64_t o) {
 #pragma unroll
-        for (int u = 0; u < kPiece / 16 / kCopyThreads; ++u)
-            if (tid + u * kCopyThreads < vecs) d[tid + u * kCopyThreads] = v[u];
+            for (int u = 0; u < U; ++u)
+                if (o + u * STEP < end) *reinterpret_cast<uint4*>(d + o + u * STEP) = q[u];
+        };
+        load(v, at);
+        for (; at < end; at += 2 * kPiece) {             // two pieces in turn: the next is on its way while one is written
+            load(w, at + kPiece);
+            store(v, at);
+            load(v, at + 2 * kPiece);
+            store(w, at + kPiece);
+        }
     }
 }
 
@@ -281,7 +314,7 @@ void set_layers(CopyParams& c, const lisa_paged_layer* layers, int n_layers) {
 // `most`: moves that there may be
 cudaError_t launch_copy(const CopyParams& c, int64_t most, cudaStream_t s) {
     const int64_t items = most * c.n_layers * c.pieces, entries = c.table ? ((int64_t)c.B * c.max_pages + kCopyThreads - 1) / kCopyThreads : 0;
-    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(std::max(items, entries), (int64_t)sm_count() * 8));
+    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(std::max(items, entries), (int64_t)sm_count() * kCopyCtas));
     const cudaError_t e = launch_chained(pages_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, s, c);
     count_launches(1);
     return e;
@@ -304,7 +337,7 @@ cudaError_t launch_pages_fork(const lisa_pages& pages, const int32_t* parent, cu
     const size_t smem = sizeof(int32_t) * (size_t)v.B * kForkCols;
     cudaError_t e = allow_smem(pages_fork_kernel, smem);
     if (e != cudaSuccess) return e;
-    e = launch_chained(pages_fork_kernel, dim3((v.max_pages + kForkCols - 1) / kForkCols + 1), dim3(256), smem, s, v, parent);
+    e = launch_chained(pages_fork_kernel, dim3((v.max_pages + kForkCols - 1) / kForkCols + 1), dim3(kForkThreads), smem, s, v, parent);
     count_launches(1);
     return e;
 }
