@@ -13,6 +13,7 @@
 // Bound by HBM: a position and head are d bytes of K and d of V.
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <type_traits>
 
 #include "paged_decode.cuh"
@@ -42,25 +43,25 @@ struct AttendParams {
 // in flight whatever the warp computes and cost no registers (with the rows of one unit ahead in registers 64 x 4096 of the 13B shape took
 // 504 us, and 307 us for V alone).  Warps never wait for one another before the end.
 // ---------------------------------------------------------------------------------------------
-constexpr int kAttendWarps = 4;
-constexpr int kAttendThreads = kAttendWarps * 32;
 constexpr int kUnit = 2;                                  // tiles that a warp takes at a time: its maximum is reduced once a unit
 constexpr int kUnitRows = kUnit * kPageBlock;
 constexpr int kBatch = 32 / kUnit;                        // units whose pages the lanes hold
 
 // A stage: K rows (or the given scores [heads][32]), V rows, {K's scale, V's scale} of each tile, whether its page is there
-// DEEP: more stages and fewer CTAs to an SM, for grids that leave it at that: a warp then has up to five units on their way.
-template <int D, int H, bool GIVEN, bool DEEP = false>
+// WIDE: eight or twelve warps to a CTA instead of four and fewer CTAs to an SM, for grids that leave it at that: a warp takes some 1700 clocks from a
+// unit's scores to its product with V, whatever comes in meanwhile, so a sequence is done sooner by more of them.
+template <int D, int H, bool GIVEN, bool WIDE>
 struct Stage {
     static constexpr int kFirst = GIVEN ? H * kUnitRows * 4 : kUnitRows * D, kV = kFirst, kScales = kV + kUnitRows * D, kThere = kScales + kUnit * 8;
     static constexpr int kBytes = kThere + 16;
-    static constexpr int kCount = DEEP ? (GIVEN && H <= 4 ? 6 : 5) : GIVEN ? 3 : 2;
+    static constexpr int kCount = GIVEN ? 3 : 2;
+    static constexpr int kWarps = !WIDE ? 4 : H > 4 || GIVEN ? 8 : 12, kThreads = kWarps * 32;
     static constexpr int kRing = kBytes * kCount;
-    static constexpr int kMerge = kAttendWarps * H * (D + 2) * 4;
-    static constexpr int kQuery = (kRing * kAttendWarps > kMerge ? kRing * kAttendWarps : kMerge);     // the queries as operands, behind the rings
+    static constexpr int kMerge = kWarps * H * (D + 2) * 4;
+    static constexpr int kQuery = (kRing * kWarps > kMerge ? kRing * kWarps : kMerge);     // the queries as operands, behind the rings
     static constexpr int kTotal = kQuery + (GIVEN ? 0 : H * (4 * D + 4));
-    static constexpr int kCtas = DEEP ? (GIVEN ? 2 : 1) : H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
-    static_assert(kCtas * (kTotal + 1024) <= 227 * 1024 + 1024, "as many CTAs as that fit an SM");
+    static constexpr int kCtas = WIDE ? (GIVEN && H <= 4 ? 2 : 1) : H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
+    static_assert(kCtas * (kTotal + 1024) <= 228 * 1024, "as many CTAs as that fit an SM");
 };
 
 // Rows lie with their 16-byte chunks permuted, so that the eight lanes of a shared-memory access meet eight different ones.  A K access is four
@@ -137,7 +138,7 @@ __device__ __forceinline__ float query_of(float* x, const AttendParams& p, int b
 template <int D, int NT, bool GIVEN>
 struct EngineF16 {
     static constexpr int H = 4 * NT, KW = D / 16, MT = D / 16;   // words of a lane per K row; tiles of 16 output columns
-    using S = Stage<D, H, GIVEN>;
+    using S = Stage<D, H, GIVEN, false>;   // (where things lie in a stage)
     uint32_t qf[GIVEN ? 1 : NT][KW][2];
     float q_scale[NT], m[NT], l[NT], o[NT][MT][4];               // m, l, q_scale: of head t
     int r_exp;                                                    // V enters as code * 2^12 scale / 2^r_exp
@@ -171,9 +172,9 @@ struct EngineF16 {
     }
 
     // The queries' terms [H][2][D] and their scales [H]: a head to a warp, brought to [2^13, 2^14) by a power of two
-    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh) {
+    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh, int warps) {
         const int lane = threadIdx.x & 31;
-        for (int j = threadIdx.x >> 5; j < H; j += kAttendWarps) {
+        for (int j = threadIdx.x >> 5; j < H; j += warps) {
             float x[D / 32];
             const float amax = query_of<D>(x, p, b, h0 + j, j < nh);
             const int ex = exponent(amax);
@@ -327,7 +328,7 @@ struct EngineF16 {
 template <int D, int NT, bool GIVEN>
 struct EngineS8 {
     static constexpr int H = 2 * NT, KS = D / 32, MT = D / 16;
-    using S = Stage<D, H, GIVEN>;
+    using S = Stage<D, H, GIVEN, false>;   // (where things lie in a stage)
     uint32_t qf[GIVEN ? 1 : NT][KS][2];
     float q_scale[NT], m[NT], l[NT], big[NT];                    // big: M; all of head 2 nt + t / 2
     int acc[NT][MT][4];
@@ -360,9 +361,9 @@ struct EngineS8 {
     }
 
     // The queries' digits [H][4][D] (the fourth is 0) and their scales [H]: a head to a warp
-    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh) {
+    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh, int warps) {
         const int lane = threadIdx.x & 31;
-        for (int j = threadIdx.x >> 5; j < H; j += kAttendWarps) {
+        for (int j = threadIdx.x >> 5; j < H; j += warps) {
             float x[D / 32];
             const float amax = query_of<D>(x, p, b, h0 + j, j < nh);
             const int ex = exponent(amax);
@@ -508,10 +509,12 @@ struct EngineS8 {
 template <int FMT, int D, int NT, bool GIVEN>
 using Engine = std::conditional_t<FMT == LISA_S8, EngineS8<D, NT, GIVEN>, EngineF16<D, NT, GIVEN>>;
 
-template <int FMT, int D, int NT, bool GIVEN, bool DEEP>
-__global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, DEEP>::kCtas) paged_attend_kernel(const __grid_constant__ AttendParams p) {
+template <int FMT, int D, int NT, bool GIVEN, bool WIDE>
+__global__ void __launch_bounds__(Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, WIDE>::kThreads, Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, WIDE>::kCtas)
+paged_attend_kernel(const __grid_constant__ AttendParams p) {
     constexpr int H = Engine<FMT, D, NT, GIVEN>::H, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
-    using S = Stage<D, H, GIVEN, DEEP>;
+    using S = Stage<D, H, GIVEN, WIDE>;
+    constexpr int kAttendWarps = S::kWarps, kAttendThreads = S::kThreads;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int kvh = blockIdx.x / p.passes, pass = blockIdx.x % p.passes;
@@ -581,7 +584,7 @@ __global__ void __launch_bounds__(kAttendThreads, Stage<D, Engine<FMT, D, NT, GI
 
     Engine<FMT, D, NT, GIVEN> engine;
     if constexpr (!GIVEN) {
-        Engine<FMT, D, NT, GIVEN>::prepare(p, smem + S::kQuery, b, h0, nh);
+        Engine<FMT, D, NT, GIVEN>::prepare(p, smem + S::kQuery, b, h0, nh, kAttendWarps);
         __syncthreads();
     }
     engine.start(smem + S::kQuery);
@@ -679,26 +682,35 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(const __grid
 }
 
 // ------------------------------------------------------------------ launches
-constexpr int kMinTiles = kUnit * kAttendWarps;           // of a CTA: less would leave warps without work
+constexpr int kMinTiles = kUnit * 4;                      // of a CTA: less would leave warps without work
 constexpr int kSplitCtas = 16;                            // CTAs an SM is given at most by splitting
 
 // Query heads that a CTA takes: two (s8) or four (e4m3) to a column tile, one or two (s8: four) of those
 int heads_per_cta(int dtype, int G) { return dtype == LISA_S8 ? (G > 4 ? 8 : G > 2 ? 4 : 2) : G > 4 ? 8 : 4; }
 
-// CTAs a sequence is split over: what per_sm CTAs an SM take, counted in tiles, each CTA with the cost of its start and end, and the merge.  Lengths are
-// on the device, where the host cannot read them: equal ones run in whole waves, and of ones spread over [L / 8, L] six tenths are left, whose CTAs fill
-// each other's gaps.  The mean of the two is what is compared, for calls with and without lengths alike, so that both give the same bits.
-int splits_for(int64_t ctas, int tiles, int per_sm, bool given) {
-    const int64_t slots = per_sm * (int64_t)sm_count(), most = std::min<int64_t>((tiles + kMinTiles - 1) / kMinTiles, kSplitCtas * (int64_t)sm_count() / ctas);
-    const double start = given ? 16 : 10, merge = given ? 32 : 16;
-    int best = 1;
+// CTAs a sequence is split over, and whether they are wide, by what they would take (us).  A tile takes what one CTA's warps need for it (`own`), or its
+// share of HBM where that is more (`share` times the CTAs of an SM); a CTA 2 us for its start and end; the merge 2.5.  Wide only where every SM has one
+// CTA at most.  Lengths are on the device, where the host cannot read them: equal ones run in waves, whose last is on average half empty, and of ones
+// spread over [L / 8, L] six tenths are left, whose CTAs fill each other's gaps.  The mean of the two is what is compared, for calls with and without lengths
+// alike, so that both give the same bits.
+// Measured (us), splits 1 | 2 | 4 | 9 | 20 narrow, then wide: 1 x 2000, 32 KV heads 15.6 | 12.9 | 9.5 | 10.0 | 10.7, 11.9 | 11.1 | 10.1 | 11.2 | 15.8; 2 x 65537, 8 KV
+// heads 521 | 268 | 184 | 101 | 57, 275 | 146 | 81 | 54 | 71; 1 x 333 6.7 and 6.2 unsplit; 16 x 2900, 32 KV heads 74 | 68 | 65 | 65 | 65, 68 | 73 | 90 | 90 | 90.
+struct Shape { int splits; bool wide; };
+template <typename Narrow, typename Wide>
+Shape shape_for(int64_t ctas, int all_tiles, bool given) {
+    const double sms = sm_count(), share = given ? 0.047 : 0.094, start = 2, merge = 2.5;
+    const int64_t most = std::min<int64_t>((all_tiles + kMinTiles - 1) / kMinTiles, kSplitCtas * (int64_t)sm_count() / ctas);
+    Shape best{1, false};
     double least = 1e300;
-    for (int s = 1; s <= std::max<int64_t>(1, most); ++s) {
-        const int64_t each = ((tiles + s - 1) / s + kMinTiles - 1) / kMinTiles * kMinTiles;
-        const double waves = 0.5 * ((double)((ctas * s + slots - 1) / slots) + std::max(1., 0.6 * (double)(ctas * s) / (double)slots));
-        const double cost = waves * ((double)each + start) + (s > 1 ? merge : 0);
-        if (cost < least) { least = cost; best = s; }
-    }
+    for (int s = 1; s <= std::max<int64_t>(1, most); ++s)
+        for (int wide = 0; wide <= (ctas * s <= sm_count()); ++wide) {
+            const double each = ((all_tiles + s - 1) / s + kMinTiles - 1) / kMinTiles * kMinTiles, per_sm = wide ? Wide::kCtas : Narrow::kCtas;
+            const double own = wide ? 0.067 : given ? 0.1 : 0.127, n = (double)(ctas * s) / sms, x = n / per_sm;
+            auto take = [&](double on_sm) { return start + each * std::max(own, share * std::min(per_sm, std::max(1., on_sm))); };
+            const double alike = std::max(1., 0.5 * (x + std::ceil(x))) * take(n), spread = std::max(1., 0.6 * x) * take(0.6 * n);
+            const double cost = 0.5 * (alike + spread) + (s > 1 ? merge : 0);
+            if (cost < least) { least = cost; best = Shape{s, wide != 0}; }
+        }
     return best;
 }
 
@@ -710,40 +722,39 @@ size_t part_bytes(int B, int Hq, int Hkv, int d, int L) {
     return (n * (2 + (size_t)d) * sizeof(float) + 255) & ~(size_t)255;
 }
 
-template <int FMT, int D, int NT, bool GIVEN>
-struct Attend {
-    template <bool DEEP>
-    static cudaError_t launch(const AttendParams& p, cudaStream_t s) {
-        using S = Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, DEEP>;
-        void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, NT, GIVEN, DEEP>;
-        const cudaError_t e = allow_smem(kernel, S::kTotal, true);
-        return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.pool.Hkv * p.passes, p.splits * p.B), dim3(kAttendThreads), S::kTotal, s, p);
-    }
-    // the deep ring where every CTA is resident with it
-    static cudaError_t launch(const AttendParams& p, cudaStream_t s) {
-        const int64_t ctas = (int64_t)p.splits * p.pool.Hkv * p.passes * p.B;
-        return ctas <= (GIVEN ? 2 : 1) * (int64_t)sm_count() ? launch<true>(p, s) : launch<false>(p, s);
-    }
-};
+template <int FMT, int D, int NT, bool GIVEN, bool WIDE>
+cudaError_t launch_one(const AttendParams& p, cudaStream_t s) {
+    using S = Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, WIDE>;
+    void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, NT, GIVEN, WIDE>;
+    const cudaError_t e = allow_smem(kernel, S::kTotal, true);
+    return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.pool.Hkv * p.passes, p.splits * p.B), dim3(S::kThreads), S::kTotal, s, p);
+}
 
-template <int FMT, bool GIVEN>
-cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
+// Shape, workspace and launch for a head width and a number of column tiles
+template <int FMT, int D, int NT, bool GIVEN>
+cudaError_t launch_sized(AttendParams& p, void* ws, cudaStream_t s) {
+    constexpr int H = Engine<FMT, D, NT, GIVEN>::H;
     const int all_tiles = (p.L + kPageBlock - 1) / kPageBlock;
-    p.heads = heads_per_cta(FMT, p.G);
-    p.passes = (p.G + p.heads - 1) / p.heads;
-    const int64_t ctas = (int64_t)p.B * p.pool.Hkv * p.passes;
-    const int splits = splits_for(ctas, all_tiles, p.heads == 8 ? Stage<128, 8, GIVEN>::kCtas : Stage<128, 4, GIVEN>::kCtas, GIVEN);
-    p.tiles = ((all_tiles + splits - 1) / splits + kMinTiles - 1) / kMinTiles * kMinTiles;
+    p.heads = H;
+    p.passes = (p.G + H - 1) / H;
+    const Shape shape = shape_for<Stage<D, H, GIVEN, false>, Stage<D, H, GIVEN, true>>((int64_t)p.B * p.pool.Hkv * p.passes, all_tiles, GIVEN);
+    p.tiles = ((all_tiles + shape.splits - 1) / shape.splits + kMinTiles - 1) / kMinTiles * kMinTiles;
     p.splits = (all_tiles + p.tiles - 1) / p.tiles;
     const size_t n = ((size_t)p.B * p.splits * p.Hq + 3) & ~(size_t)3;     // (not used where nothing is split)
     p.ws_m = static_cast<float*>(ws);
     p.ws_l = p.ws_m + n;
     p.ws_o = p.ws_l + n;
+    return shape.wide ? launch_one<FMT, D, NT, GIVEN, true>(p, s) : launch_one<FMT, D, NT, GIVEN, false>(p, s);
+}
+
+template <int FMT, bool GIVEN>
+cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
+    const int heads = heads_per_cta(FMT, p.G);
     auto attend = [&](auto width) -> cudaError_t {
         constexpr int D = decltype(width)::value, per = FMT == LISA_S8 ? 2 : 4;
         if constexpr (FMT == LISA_S8)
-            if (p.heads == 2) return Attend<FMT, D, 1, GIVEN>::launch(p, s);
-        return p.heads == 4 ? Attend<FMT, D, 4 / per, GIVEN>::launch(p, s) : Attend<FMT, D, 8 / per, GIVEN>::launch(p, s);
+            if (heads == 2) return launch_sized<FMT, D, 1, GIVEN>(p, ws, s);
+        return heads == 4 ? launch_sized<FMT, D, 4 / per, GIVEN>(p, ws, s) : launch_sized<FMT, D, 8 / per, GIVEN>(p, ws, s);
     };
     cudaError_t e = p.pool.d == 128 ? attend(std::integral_constant<int, 128>{}) : p.pool.d == 64 ? attend(std::integral_constant<int, 64>{})
                                                                                                     : attend(std::integral_constant<int, 32>{});

@@ -260,12 +260,11 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     uint8_t* ring = smem_b + lay.ring + warp * kRingHeads * lay.stage;
     chain_release();
     // the aligner's weights are constants of the model: staged while the kernel before this one may still be running
-    const int c8 = mp / 8;
-    for (int e = tid; e < KS1 * 16 * c8; e += THREADS) {
-        const int k = e / c8, c = (e - k * c8) * 8;
-        const bool in = k < (CONCAT ? 2 * HQ : HQ) && c < m;
-        cp_async<16>((uint32_t)__cvta_generic_to_shared(w1_s + k * w1_ld + c), static_cast<const __nv_bfloat16*>(p.w1) + (in ? k * m + c : 0), in);
-    }
+    for (int k = warp; k < KS1 * 16; k += NW)
+        for (int c = lane * 8; c < mp; c += 256) {
+            const bool in = k < (CONCAT ? 2 * HQ : HQ) && c < m;
+            cp_async<16>((uint32_t)__cvta_generic_to_shared(w1_s + k * w1_ld + c), static_cast<const __nv_bfloat16*>(p.w1) + (in ? k * m + c : 0), in);
+        }
     for (int e = tid; e < mp * NT2; e += THREADS) {
         const int k = e / NT2, c = e % NT2 * 8;
         cp_async<16>((uint32_t)__cvta_generic_to_shared(w2_s + k * W2_LD + c), static_cast<const __nv_bfloat16*>(p.w2) + (k < m ? k * HQ + c : 0), k < m);
@@ -471,13 +470,27 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y_s[(hs * HQ + j * 8 + 2 * t + (e & 1)) * LD + (e & 2 ? p1 : p0)] = yacc[j][e];
             __syncthreads();
-            for (int e = tid; e < HQ * CH; e += THREADS) {
-                const int h = e / CH, pos = e % CH;
-                if (j0 + pos >= L || !(there >> (pos / kPageBlock) & 1)) continue;
-                float x = CONCAT ? 0.f : s_s[h * LD + pos];
+            // a thread has one position and every THREADS / CH-th head
+            const int pos = tid % CH, h0 = tid / CH;
+            if (j0 + pos < L && (there >> (pos / kPageBlock) & 1)) {
+                const float* y = y_s + h0 * LD + pos;
+                auto finish = [&](auto* row, int64_t sb, int64_t sh) {
+                    row += b * sb + h0 * sh + j0 + pos;
+                    sh *= THREADS / CH;
 #pragma unroll
-                for (int q = 0; q < HS; ++q) x += y_s[(q * HQ + h) * LD + pos];
-                put_score(p, b, h, j0 + pos, x);
+                    for (int h = 0; h < HQ; h += THREADS / CH, row += sh) {
+                        if (HQ % (THREADS / CH) != 0 && h0 + h >= HQ) break;
+                        float x = CONCAT ? 0.f : s_s[(h0 + h) * LD + pos];
+#pragma unroll
+                        for (int q = 0; q < HS; ++q) x += y[(q * HQ + h) * LD];
+                        *row = to_row<std::remove_pointer_t<decltype(row)>>(x);
+                    }
+                };
+                finish(p.scores, p.s_sb, p.s_sh);
+                if (p.out_scores) {
+                    if (p.row_bf16) finish(static_cast<__nv_bfloat16*>(p.out_scores), p.sc_sb, p.sc_sh);
+                    else finish(static_cast<float*>(p.out_scores), p.sc_sb, p.sc_sh);
+                }
             }
         }
         if (chunk + 1 == chunks) break;
@@ -491,13 +504,15 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
 template <int FMT, int HQ, bool CONCAT>
 cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
     // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128.  Fewer positions where that
-    // does not give the SMs one and a half.  Eight tenths of the CTAs are taken to have positions (all, where lengths are alike, or six tenths, where they
+    // does not give the SMs one and a half (three, and then three quarters, of the concatenating form, whose CTAs take longest).  Eight tenths of the CTAs are taken to have positions (all, where lengths are alike, or six tenths, where they
     // are spread over [L / 8, L]).
     constexpr int NW = CONCAT ? 8 : 4;
     constexpr double fill = 0.8;
-    int ch = CONCAT ? 64 : NW * 16;
-    if (CONCAT && fill * p.B * ((p.L + 127) / 128) >= 4 * sm_count()) ch = 128;
-    while (ch > 16 && fill * p.B * ((p.L + ch - 1) / ch) < 1.5 * sm_count()) ch /= 2;
+    auto ctas = [&](int c) { return fill * p.B * ((p.L + c - 1) / c); };
+    int ch = 64;
+    if (CONCAT && ctas(128) >= 4 * sm_count()) ch = 128;
+    else if (CONCAT && ctas(64) < 3 * sm_count()) ch = 32;
+    while (ch > 16 && ctas(ch) < (CONCAT ? 0.75 : 1.5) * sm_count()) ch /= 2;
     void (*kernel)(ScoresParams, int) = ch == 64 ? paged_scores_kernel<FMT, HQ, NW, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, NW, 32, CONCAT>
                                                                                                : paged_scores_kernel<FMT, HQ, NW, 16, CONCAT>;
     if constexpr (CONCAT)
