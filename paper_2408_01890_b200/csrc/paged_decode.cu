@@ -4,10 +4,10 @@
 // running maximum and sum: a warp streams its tiles of 16 positions (a tile never leaves a page) and keeps everything in registers; warps,
 // and where a sequence is split CTAs, are joined at the end.
 //
-// Both products over codes run on mma.sync m16n8k16 with the codes as the A operand, as fp16, which holds them exactly; scales are applied to the
-// fp32 results.  The other operand is q or the probabilities, brought to [2^13, 2^15) by a power of two and split into two fp16 terms (22 bits)
-// that take two neighbouring columns of B, so that the eight columns are four query heads: with few heads to a KV head the columns
-// are there anyway.  The sum of the two columns is what an fp32 product would give, up to 2^-22 of the largest term.
+// Both products over codes run on mma.sync with the codes as the A operand, which no engine rounds (s8 and e4m3 codes as they are, or as fp16); scales are
+// applied to the fp32 or integer results.  The other operand, q or the probabilities, is split into terms or digits that take neighbouring columns of B: the eight
+// columns are one to four query heads, and where few heads share a KV head the columns are there anyway.  Their sum is what an fp32 product would give,
+// up to 2^-22 of the largest term.
 // The order of d in q.K, of d in the rows of the output, and of positions in P.V is free, so every lane's share of a fragment is 16 consecutive
 // bytes of a row.
 // Bound by HBM: a position and head are d bytes of K and d of V.
@@ -59,7 +59,7 @@ struct Stage {
     static constexpr int kRing = kBytes * kCount;
     static constexpr int kMerge = kWarps * H * (D + 2) * 4;
     static constexpr int kQuery = (kRing * kWarps > kMerge ? kRing * kWarps : kMerge);     // the queries as operands, behind the rings
-    static constexpr int kTotal = kQuery + (GIVEN ? 0 : H * (4 * D + 4));
+    static constexpr int kTotal = kQuery + (GIVEN ? 0 : H * (8 * D + 4));
     static constexpr int kCtas = WIDE ? (GIVEN && H <= 4 ? 2 : 1) : H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
     static_assert(kCtas * (kTotal + 1024) <= 228 * 1024, "as many CTAs as that fit an SM");
 };
@@ -134,7 +134,7 @@ __device__ __forceinline__ float query_of(float* x, const AttendParams& p, int b
 
 // The arithmetic of a warp over its units.  Shared memory of a stage: st; pos0: the unit's first position; there: bit u: tile u's page is there.
 //
-// e4m3: products on mma m16n8k16 fp16, where every code is exact; the other operand as two fp16 terms, so that the eight columns are four heads.
+// e4m3 with three or more heads to a KV head: products on mma m16n8k16 fp16, where every code is exact; the other operand as two fp16 terms, so that the eight columns are four heads.
 template <int D, int NT, bool GIVEN>
 struct EngineF16 {
     static constexpr int H = 4 * NT, KW = D / 16, MT = D / 16;   // words of a lane per K row; tiles of 16 output columns
@@ -157,7 +157,7 @@ struct EngineF16 {
         }
         if constexpr (!GIVEN) {   // column g is head g / 2's leading (even g) or second term
             const __half* q = reinterpret_cast<const __half*>(q_s);
-            const float* scale = reinterpret_cast<const float*>(q_s + H * 4 * D);
+            const float* scale = reinterpret_cast<const float*>(q_s + H * 8 * D);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int j = nt * 4 + (g >> 1);
@@ -186,7 +186,7 @@ struct EngineF16 {
                 q[e] = hi;
                 q[D + e] = __float2half_rn(x[e] * up - __half2float(hi));
             }
-            if (lane == 0) reinterpret_cast<float*>(q_s + H * 4 * D)[j] = pow2(ex - 13) * rsqrtf((float)D);
+            if (lane == 0) reinterpret_cast<float*>(q_s + H * 8 * D)[j] = pow2(ex - 13) * rsqrtf((float)D);
         }
     }
 
@@ -349,7 +349,7 @@ struct EngineS8 {
             }
         }
         if constexpr (!GIVEN) {   // columns 0, 1, 2: head 0's digits, most significant first; 4, 5, 6: head 1's
-            const float* scale = reinterpret_cast<const float*>(q_s + H * 4 * D);
+            const float* scale = reinterpret_cast<const float*>(q_s + H * 8 * D);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -378,7 +378,7 @@ struct EngineS8 {
                 q[e] = (uint8_t)((v - mid) >> 8); q[D + e] = (uint8_t)mid; q[2 * D + e] = (uint8_t)lo; q[3 * D + e] = 0;
             }
             // (a query that is not finite has no digits: its scores are NaN)
-            if (lane == 0) reinterpret_cast<float*>(q_s + H * 4 * D)[j] = amax < INFINITY ? pow2(max(ex - 21, -126)) * rsqrtf((float)D) : __uint_as_float(0x7fc00000u);
+            if (lane == 0) reinterpret_cast<float*>(q_s + H * 8 * D)[j] = amax < INFINITY ? pow2(max(ex - 21, -126)) * rsqrtf((float)D) : __uint_as_float(0x7fc00000u);
         }
     }
 
@@ -506,13 +506,160 @@ struct EngineS8 {
     }
 };
 
-template <int FMT, int D, int NT, bool GIVEN>
-using Engine = std::conditional_t<FMT == LISA_S8, EngineS8<D, NT, GIVEN>, EngineF16<D, NT, GIVEN>>;
+// e4m3 with one or two heads to a KV head: products on mma m16n8k32 e4m3, the codes as they are; the other operand in fixed point as for s8, its 24 bits
+// as six base-16 digits that are codes themselves (Base16) and take six of a head's eight columns.  A lane holds the score of position g + 8 (t % 2) of tile t / 2.
+template <int D, int NT, bool GIVEN>
+struct EngineE4M3 {
+    static constexpr int H = NT, KS = D / 32, MT = D / 16;
+    using S = Stage<D, H, GIVEN, false>;   // (where things lie in a stage)
+    uint32_t qf[GIVEN ? 1 : NT][KS][2];
+    float q_scale[NT], m[NT], l[NT], big[NT], o[NT][MT][4];      // o: over e^M / 2^13
 
-template <int FMT, int D, int NT, bool GIVEN, bool WIDE>
-__global__ void __launch_bounds__(Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, WIDE>::kThreads, Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, WIDE>::kCtas)
+    __device__ __forceinline__ void start(const uint8_t* q_s) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt] = big[nt] = -INFINITY;
+            l[nt] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
+            if constexpr (!GIVEN) {
+#pragma unroll
+                for (int w = 0; w < 2 * KS; ++w) qf[nt][w >> 1][w & 1] = *reinterpret_cast<const uint32_t*>(q_s + (nt * 8 + g) * D + k_column<D>(w, t));
+                q_scale[nt] = reinterpret_cast<const float*>(q_s + H * 8 * D)[nt];
+            }
+        }
+    }
+
+    // The queries' digits [H][8][D] (the last two are 0), signs in every one, and their scales [H]: a head to a warp
+    static __device__ __forceinline__ void prepare(const AttendParams& p, uint8_t* q_s, int b, int h0, int nh, int warps) {
+        const int lane = threadIdx.x & 31;
+        for (int j = threadIdx.x >> 5; j < H; j += warps) {
+            float x[D / 32];
+            const float amax = query_of<D>(x, p, b, h0 + j, j < nh);
+            const int ex = exponent(amax);
+            const float up = pow2(min(21 - ex, 127));
+            uint8_t* q = q_s + j * 8 * D + lane * (D / 32);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) {
+                const uint32_t v = __float2uint_rn(fabsf(x[e]) * up), sign = __float_as_uint(x[e]) >> 24 & 0x80u;    // v <= 2^22
+#pragma unroll
+                for (int i = 0; i < 6; ++i) q[i * D + e] = (uint8_t)(sign | (v >> (20 - 4 * i) & 15u));
+                q[6 * D + e] = q[7 * D + e] = 0;
+            }
+            if (lane == 0) reinterpret_cast<float*>(q_s + H * 8 * D)[j] = amax < INFINITY ? pow2(max(ex - 12, -126)) * rsqrtf((float)D) : __uint_as_float(0x7fc00000u);
+        }
+    }
+
+    __device__ __forceinline__ void unit(const AttendParams& p, const uint8_t* st, int pos0, int L, int b, int h0, int nh) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, at = (t >> 1) * kPageBlock + g + 8 * (t & 1);
+        const float2 sc = reinterpret_cast<const float2*>(st + S::kScales)[t >> 1];
+        const float lv = __log2f(sc.y);
+        const bool on = reinterpret_cast<const int*>(st + S::kThere)[t >> 1] && pos0 + at < L;
+        float s[NT];
+        if constexpr (!GIVEN) {
+            const Base16 base(t);
+            float c[kUnit][NT][4];
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) {
+                uint32_t kw[2][2 * KS];
+                load_k<D>(kw, st, u);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) c[u][nt][0] = c[u][nt][1] = c[u][nt][2] = c[u][nt][3] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        mma_e4m3(c[u][nt], kw[0][2 * ks], kw[1][2 * ks], kw[0][2 * ks + 1], kw[1][2 * ks + 1], qf[nt][ks][0], qf[nt][ks][1]);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt] = base.scatter(c[0][nt], c[1][nt], t) * (sc.x * q_scale[nt]);
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt] = nt < nh ? reinterpret_cast<const float*>(st)[nt * kUnitRows + at] : 0.f;
+        }
+        bool grown = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (!GIVEN && p.out_scores && on && nt < nh) put_row(p, b, h0 + nt, pos0 + at, s[nt]);
+            s[nt] = on ? s[nt] * kLog2e : -INFINITY;
+            grown |= s[nt] > m[nt] + 2.f || s[nt] + lv > big[nt] + 1.99f;
+        }
+        if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float mx = fmaxf(m[nt], s[nt]), bg = fmaxf(big[nt], s[nt] + lv);
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                    bg = fmaxf(bg, __shfl_xor_sync(0xffffffffu, bg, off));
+                }
+                l[nt] *= mx == -INFINITY ? 1.f : exp2_(m[nt] - mx);
+                const float f = bg == -INFINITY ? 1.f : exp2_(big[nt] - bg);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
+                m[nt] = mx;
+                big[nt] = bg;
+            }
+        }
+        uint32_t bf[NT][kUnit];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float ref = m[nt] == -INFINITY ? 0.f : m[nt], w_ref = big[nt] == -INFINITY ? 0.f : big[nt];
+            l[nt] += fmaf(sc.y, 0.f, exp2_(s[nt] - ref));                    // (a scale that is NaN reaches the output through the sum)
+            const uint32_t w = __float2uint_rn(exp2_(s[nt] + lv - w_ref) * 4194304.f);
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) {
+                uint32_t d[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {             // rows of a matrix: positions g + 8 e; lane t has byte 2 - t, its two digits
+                    const uint32_t v = __byte_perm(__shfl_sync(0xffffffffu, w, (lane & 28) | (2 * u + e)), 0u, 0x4440 + (t == 3 ? 4 : 2 - t));
+                    d[e] = transpose8x8((v >> 4) | (v & 15u) << 16);
+                }
+                bf[nt][u] = __byte_perm(d[0], d[1], 0x6420);  // column g's digits at positions 2t, 2t + 1, 2t + 8, 2t + 9
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < MT; c += 2) {
+            uint32_t v[kUnit][4];
+#pragma unroll
+            for (int u = 0; u < kUnit; ++u) load_v<D>(v[u], st + S::kV, u, c);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t a0 = __byte_perm(v[0][2 * x], v[0][2 * x + 1], 0x6420), a1 = __byte_perm(v[0][2 * x], v[0][2 * x + 1], 0x7531);
+                const uint32_t a2 = __byte_perm(v[1][2 * x], v[1][2 * x + 1], 0x6420), a3 = __byte_perm(v[1][2 * x], v[1][2 * x + 1], 0x7531);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_e4m3(o[nt][c + x], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void finish(float* s_m, float* s_l, float* s_o) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const Base16 base(t);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float f = big[nt] == -INFINITY ? 0.f : exp2_(big[nt] - m[nt]) * (1.f / 8192.f);
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) l[nt] += __shfl_xor_sync(0xffffffffu, l[nt], off);
+            if (lane == 0) { s_m[nt] = m[nt]; s_l[nt] = l[nt]; }
+#pragma unroll
+            for (int c = 0; c < MT; c += 2) s_o[nt * D + 16 * (c + (t >> 1)) + 2 * g + (t & 1)] = base.scatter(o[nt][c], o[nt][c + 1], t) * f;
+        }
+    }
+};
+
+// The engine of a type and of up to HEADS query heads (1, s8: 2; 2, 4 or 8) to a KV head
+template <int FMT, int D, int HEADS, bool GIVEN>
+using Engine = std::conditional_t<FMT == LISA_S8, EngineS8<D, (HEADS + 1) / 2, GIVEN>,
+                                  std::conditional_t<(HEADS <= 2), EngineE4M3<D, HEADS, GIVEN>, EngineF16<D, (HEADS + 3) / 4, GIVEN>>>;
+
+template <int FMT, int D, int HEADS, bool GIVEN, bool WIDE>
+__global__ void __launch_bounds__(Stage<D, Engine<FMT, D, HEADS, GIVEN>::H, GIVEN, WIDE>::kThreads, Stage<D, Engine<FMT, D, HEADS, GIVEN>::H, GIVEN, WIDE>::kCtas)
 paged_attend_kernel(const __grid_constant__ AttendParams p) {
-    constexpr int H = Engine<FMT, D, NT, GIVEN>::H, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
+    constexpr int H = Engine<FMT, D, HEADS, GIVEN>::H, LPR = D / 16, RPI = 32 / LPR;   // lanes that copy a row, rows that a warp copies at once
     using S = Stage<D, H, GIVEN, WIDE>;
     constexpr int kAttendWarps = S::kWarps, kAttendThreads = S::kThreads;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -582,9 +729,9 @@ paged_attend_kernel(const __grid_constant__ AttendParams p) {
 #pragma unroll
     for (int i = 0; i < S::kCount - 1; ++i) ask(i, i);
 
-    Engine<FMT, D, NT, GIVEN> engine;
+    Engine<FMT, D, HEADS, GIVEN> engine;
     if constexpr (!GIVEN) {
-        Engine<FMT, D, NT, GIVEN>::prepare(p, smem + S::kQuery, b, h0, nh, kAttendWarps);
+        Engine<FMT, D, HEADS, GIVEN>::prepare(p, smem + S::kQuery, b, h0, nh, kAttendWarps);
         __syncthreads();
     }
     engine.start(smem + S::kQuery);
@@ -685,8 +832,8 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(const __grid
 constexpr int kMinTiles = kUnit * 4;                      // of a CTA: less would leave warps without work
 constexpr int kSplitCtas = 16;                            // CTAs an SM is given at most by splitting
 
-// Query heads that a CTA takes: two (s8) or four (e4m3) to a column tile, one or two (s8: four) of those
-int heads_per_cta(int dtype, int G) { return dtype == LISA_S8 ? (G > 4 ? 8 : G > 2 ? 4 : 2) : G > 4 ? 8 : 4; }
+// Query heads that a CTA takes at most of a KV head's G
+int heads_per_cta(int dtype, int G) { return G > 4 ? 8 : G > 2 ? 4 : dtype == LISA_S8 ? 2 : G; }
 
 // CTAs a sequence is split over, and whether they are wide, by what they would take (us).  A tile takes what one CTA's warps need for it (`own`), or its
 // share of HBM where that is more (`share` times the CTAs of an SM); a CTA 2 us for its start and end; the merge 2.5.  Wide only where every SM has one
@@ -722,18 +869,18 @@ size_t part_bytes(int B, int Hq, int Hkv, int d, int L) {
     return (n * (2 + (size_t)d) * sizeof(float) + 255) & ~(size_t)255;
 }
 
-template <int FMT, int D, int NT, bool GIVEN, bool WIDE>
+template <int FMT, int D, int HEADS, bool GIVEN, bool WIDE>
 cudaError_t launch_one(const AttendParams& p, cudaStream_t s) {
-    using S = Stage<D, Engine<FMT, D, NT, GIVEN>::H, GIVEN, WIDE>;
-    void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, NT, GIVEN, WIDE>;
+    using S = Stage<D, Engine<FMT, D, HEADS, GIVEN>::H, GIVEN, WIDE>;
+    void (*kernel)(AttendParams) = paged_attend_kernel<FMT, D, HEADS, GIVEN, WIDE>;
     const cudaError_t e = allow_smem(kernel, S::kTotal, true);
     return e != cudaSuccess ? e : launch_chained(kernel, dim3(p.pool.Hkv * p.passes, p.splits * p.B), dim3(S::kThreads), S::kTotal, s, p);
 }
 
-// Shape, workspace and launch for a head width and a number of column tiles
-template <int FMT, int D, int NT, bool GIVEN>
+// Shape, workspace and launch for a head width and a number of heads
+template <int FMT, int D, int HEADS, bool GIVEN>
 cudaError_t launch_sized(AttendParams& p, void* ws, cudaStream_t s) {
-    constexpr int H = Engine<FMT, D, NT, GIVEN>::H;
+    constexpr int H = Engine<FMT, D, HEADS, GIVEN>::H;
     const int all_tiles = (p.L + kPageBlock - 1) / kPageBlock;
     p.heads = H;
     p.passes = (p.G + H - 1) / H;
@@ -744,17 +891,19 @@ cudaError_t launch_sized(AttendParams& p, void* ws, cudaStream_t s) {
     p.ws_m = static_cast<float*>(ws);
     p.ws_l = p.ws_m + n;
     p.ws_o = p.ws_l + n;
-    return shape.wide ? launch_one<FMT, D, NT, GIVEN, true>(p, s) : launch_one<FMT, D, NT, GIVEN, false>(p, s);
+    return shape.wide ? launch_one<FMT, D, HEADS, GIVEN, true>(p, s) : launch_one<FMT, D, HEADS, GIVEN, false>(p, s);
 }
 
 template <int FMT, bool GIVEN>
 cudaError_t launch_attend(AttendParams& p, void* ws, cudaStream_t s) {
     const int heads = heads_per_cta(FMT, p.G);
     auto attend = [&](auto width) -> cudaError_t {
-        constexpr int D = decltype(width)::value, per = FMT == LISA_S8 ? 2 : 4;
-        if constexpr (FMT == LISA_S8)
-            if (heads == 2) return launch_sized<FMT, D, 1, GIVEN>(p, ws, s);
-        return heads == 4 ? launch_sized<FMT, D, 4 / per, GIVEN>(p, ws, s) : launch_sized<FMT, D, 8 / per, GIVEN>(p, ws, s);
+        constexpr int D = decltype(width)::value;
+        if (heads == 8) return launch_sized<FMT, D, 8, GIVEN>(p, ws, s);
+        if (heads == 4) return launch_sized<FMT, D, 4, GIVEN>(p, ws, s);
+        if constexpr (FMT == LISA_E4M3)
+            if (heads == 1) return launch_sized<FMT, D, 1, GIVEN>(p, ws, s);
+        return launch_sized<FMT, D, 2, GIVEN>(p, ws, s);
     };
     cudaError_t e = p.pool.d == 128 ? attend(std::integral_constant<int, 128>{}) : p.pool.d == 64 ? attend(std::integral_constant<int, 64>{})
                                                                                                     : attend(std::integral_constant<int, 32>{});

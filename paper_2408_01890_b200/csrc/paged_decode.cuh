@@ -26,27 +26,26 @@ __device__ __forceinline__ bool deal_item(const int32_t* seq_lens, int B, int L,
         const int s = q * 32 + lane;
         lens[q] = s < B ? length_of(seq_lens, s, L) : -1;
     }
+    bool found = false;
 #pragma unroll
-    for (int q = 0; q < kDealMaxB / 32; ++q) {
-        if (q * 32 >= B) break;
-        const int n = lens[q] < 0 ? 0 : max(least, (lens[q] + unit - 1) / unit);
-        int upto = n;
+    for (int q = 0; q < kDealMaxB / 32; ++q)
+        if (q * 32 < B && !found) {
+            const int n = lens[q] < 0 ? 0 : max(least, (lens[q] + unit - 1) / unit);
+            int upto = n;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const uint32_t above = __ballot_sync(0xffffffffu, upto > left);
-        if (above) {
-            const int src = __ffs(above) - 1;
-            b = q * 32 + src;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            const uint32_t above = __ballot_sync(0xffffffffu, upto > left);
+            found = above != 0;
+            const int src = found ? __ffs(above) - 1 : 31;
+            b = __shfl_sync(0xffffffffu, q * 32 + src, 0);       // (uniform, as the compiler sees it)
             part = __shfl_sync(0xffffffffu, left - (upto - n), src);
             len = __shfl_sync(0xffffffffu, lens[q], src);
-            return true;
+            left -= __shfl_sync(0xffffffffu, upto, 31);
         }
-        left -= __shfl_sync(0xffffffffu, upto, 31);
-    }
-    return false;
+    return found;
 }
 
 // d += a (16x16, row) . b (16x8, col), fp16 in, fp32 accumulate
@@ -72,6 +71,29 @@ __device__ __forceinline__ float digits_sum(const int* c, bool odd) {
     const float x = fmaf((float)c[0], f0, (float)c[1] * f1), y = fmaf((float)c[2], f0, (float)c[3] * f1);
     return (odd ? y : x) + __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
 }
+// d += a (16x32, row) . b (32x8, col), e4m3, fp32 accumulate
+__device__ __forceinline__ void mma_e4m3(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// An e4m3 product whose second operand are base-16 digits: the byte n is e4m3's n 2^-9 for n in 0 .. 15 (subnormals and the first binade lie evenly), so the
+// nibbles of a 24-bit number are six columns, most significant first.  What the columns 2t, 2t + 1 of a sum weigh:
+struct Base16 {
+    float w0, w1;
+    __device__ __forceinline__ explicit Base16(int t) {
+        w0 = t == 0 ? 1048576.f : t == 1 ? 4096.f : t == 2 ? 16.f : 0.f;
+        w1 = t == 0 ? 65536.f : t == 1 ? 256.f : t == 2 ? 1.f : 0.f;
+    }
+    __device__ __forceinline__ float operator()(float c0, float c1) const { return fmaf(c0, w0, c1 * w1); }
+    // Sums over the four lanes t of rows g and g + 8 of two products: lane t ends up with row g + 8 (t % 2) of product t / 2
+    __device__ __forceinline__ float scatter(const float* a, const float* b, int t) const {
+        const bool second = t & 2, low = t & 1;
+        const float a0 = (*this)(a[0], a[1]), a1 = (*this)(a[2], a[3]), b0 = (*this)(b[0], b[1]), b1 = (*this)(b[2], b[3]);
+        const float x = (second ? b0 : a0) + __shfl_xor_sync(0xffffffffu, second ? a0 : b0, 2);
+        const float y = (second ? b1 : a1) + __shfl_xor_sync(0xffffffffu, second ? a1 : b1, 2);
+        return (low ? y : x) + __shfl_xor_sync(0xffffffffu, low ? x : y, 1);
+    }
+};
 // fp16 mma with k = 8
 __device__ __forceinline__ void mma_f16_k8(float* d, uint32_t a0, uint32_t a1, uint32_t b0) {
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
