@@ -54,13 +54,13 @@ template <int D, int H, bool GIVEN, bool WIDE>
 struct Stage {
     static constexpr int kFirst = GIVEN ? H * kUnitRows * 4 : kUnitRows * D, kV = kFirst, kScales = kV + kUnitRows * D, kThere = kScales + kUnit * 8;
     static constexpr int kBytes = kThere + 16;
-    static constexpr int kCount = GIVEN ? 3 : 2;
+    static constexpr int kCount = !GIVEN ? 2 : H > 4 || WIDE ? 3 : 4;
     static constexpr int kWarps = !WIDE ? 4 : H > 4 || GIVEN ? 8 : 12, kThreads = kWarps * 32;
     static constexpr int kRing = kBytes * kCount;
     static constexpr int kMerge = kWarps * H * (D + 2) * 4;
     static constexpr int kQuery = (kRing * kWarps > kMerge ? kRing * kWarps : kMerge);     // the queries as operands, behind the rings
     static constexpr int kTotal = kQuery + (GIVEN ? 0 : H * (8 * D + 4));
-    static constexpr int kCtas = WIDE ? (GIVEN && H <= 4 ? 2 : 1) : H > 4 ? 2 : GIVEN ? 4 : 3;   // an SM's, by registers and by 227 KB
+    static constexpr int kCtas = WIDE ? (GIVEN && H <= 4 ? 2 : 1) : H > 4 ? 2 : 3;   // an SM's, by registers and by 227 KB
     static_assert(kCtas * (kTotal + 1024) <= 228 * 1024, "as many CTAs as that fit an SM");
 };
 
