@@ -1,0 +1,117 @@
+"""Serving from a paged 8-bit cache: sequences that come, grow, branch and leave, through the library's paged entry points.
+
+A PagedDecoder holds the pages of a stack of layers and B rows, each a sequence or an idle slot.  Prompts are admitted to rows, a step
+gives every row that has a sequence one more token, fork lets rows take over one another's sequences (a beam search's step; nothing is copied before one
+of them writes), release frees rows, and compact moves the pages in use to the front of the pools.  Lengths and tables live on the device: a step
+makes no copy to the host and can be captured in a CUDA graph.  The projections that give Q, K and V lie outside, as in stack.py; all
+arithmetic runs in the library's kernels.
+
+    python -m paper_2408_01890_b200.serving        a small run on synthetic tensors
+"""
+from __future__ import annotations
+
+from typing import List, Optional, Sequence, Tuple
+
+import torch
+
+from . import binding as lb
+
+
+class PagedDecoder:
+    def __init__(self, kinds: Sequence[int], weights: Sequence[Optional[Tuple[torch.Tensor, torch.Tensor]]], *, rows: int, n_pages: int,
+                 max_len: int, Hq: int, Hkv: int, d: int, r: int, page_tokens: int = 64, dtype: int = lb.S8, act: int = lb.ACT_RELU):
+        """kinds[l]: CACHE_STANDARD or CACHE_SHARED; weights[l]: a shared layer's aligner (w1, w2).  max_len bounds a sequence's length."""
+        assert kinds[0] == lb.CACHE_STANDARD, "layer 0 has no previous scores to share"
+        max_pages = -(-max_len // page_tokens)
+        self.kinds, self.weights, self.Hq, self.act = list(kinds), list(weights), Hq, act
+        self.L = max_pages * page_tokens
+        self.cache = lb.PagedCache(kinds, n_pages, Hkv, page_tokens, d, r, dtype=dtype)
+        self.pages = lb.Pages.empty(rows, max_pages, n_pages, page_tokens)
+        self.scores = [torch.empty((rows, Hq, self.L), dtype=torch.float32, device="cuda") for _ in range(2)]
+        self.workspace = {k: lb.paged_decode_workspace(self.cache.layers[self.kinds.index(k)], rows, Hq, self.L) for k in set(kinds)}
+
+    @property
+    def lens(self) -> torch.Tensor:
+        return self.pages.lens
+
+    def admit(self, rows_kv: Sequence[Tuple[torch.Tensor, torch.Tensor]], counts: torch.Tensor) -> None:
+        """counts[b] more positions for row b, of which rows_kv[l] = (K or K' [B,n,Hkv,d|r], V [B,n,Hkv,d]) are layer l's."""
+        lb.lisa_pages_reserve(self.pages, self.cache, counts)
+        for layer, (k, v) in zip(self.cache.layers, rows_kv):
+            lb.lisa_paged_append(layer, self.pages.table, k, v, self.pages.lens, counts)
+        self.pages.lens.add_(counts)
+
+    def step(self, tokens: Sequence[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]], outs: Sequence[torch.Tensor]) -> None:
+        """One token for every row that has a sequence.  tokens[l]: (Q or Q' [B,1,Hq,d|r], K or K', V); outs[l] [B,1,Hq,d] (zeros in idle rows)."""
+        active = (self.pages.lens > 0).to(torch.int32)
+        self.admit([t[1:] for t in tokens], active)
+        row = 0
+        for l, (kind, layer) in enumerate(zip(self.kinds, self.cache.layers)):
+            shared_next = l + 1 < len(self.kinds) and self.kinds[l + 1] == lb.CACHE_SHARED
+            kept = self.scores[row ^ 1] if shared_next else None
+            call = dict(L=self.L, seq_lens=self.pages.lens, out=outs[l], out_scores=kept, workspace=self.workspace[kind])
+            if kind == lb.CACHE_STANDARD:
+                lb.lisa_attn_anchor_paged(tokens[l][0], layer, self.pages.table, **call)
+            else:
+                w1, w2 = self.weights[l]
+                lb.lisa_attn_shared_decode_paged(self.scores[row], lb.Link(tokens[l][0], None, w1, w2, act=self.act), layer, self.pages.table, **call)
+            row ^= shared_next
+
+    def fork(self, parent: torch.Tensor) -> None:
+        """Row i goes on with the sequence of row parent[i] (int32 on the device); -1 frees it."""
+        lb.lisa_pages_fork(self.pages, parent)
+
+    def release(self, rows: Sequence[int]) -> None:
+        parent = torch.arange(self.pages.lens.shape[0], dtype=torch.int32)
+        parent[list(rows)] = -1
+        self.fork(parent.cuda())
+
+    def compact(self) -> None:
+        lb.lisa_pages_compact(self.pages, self.cache)
+
+
+def _tokens(kinds: Sequence[int], B: int, n: int, Hq: int, Hkv: int, d: int, r: int, g: torch.Generator) -> List[Tuple[torch.Tensor, ...]]:
+    def draw(*shape):
+        return torch.randn(shape, generator=g, device="cuda").bfloat16()
+    width = [r if k == lb.CACHE_SHARED else d for k in kinds]
+    return [(draw(B, n, Hq, w), draw(B, n, Hkv, w), draw(B, n, Hkv, d)) for w in width]
+
+
+def main() -> None:
+    """Prompts of unlike lengths, decoding replayed from a graph, a beam step between replays, and a compaction at the end."""
+    B, Hq, Hkv, d, r, m, P, steps = 16, 32, 8, 128, 21, 64, 64, 64
+    kinds = [lb.CACHE_STANDARD, lb.CACHE_SHARED, lb.CACHE_SHARED, lb.CACHE_SHARED] * 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    weights = [None if k == lb.CACHE_STANDARD else ((torch.randn((Hq, m), generator=g, device="cuda") * Hq ** -0.5).bfloat16(),
+                                                    (torch.randn((m, Hq), generator=g, device="cuda") * m ** -0.5).bfloat16()) for k in kinds]
+    max_len = 1536
+    dec = PagedDecoder(kinds, weights, rows=B, n_pages=B * (max_len // P) + B, max_len=max_len, Hq=Hq, Hkv=Hkv, d=d, r=r, page_tokens=P)
+    counts = torch.randint(1, 1024, (B,), generator=g, device="cuda", dtype=torch.int32)
+    prompt = _tokens(kinds, B, 1024, Hq, Hkv, d, r, g)
+    dec.admit([t[1:] for t in prompt], counts)
+    token = _tokens(kinds, B, 1, Hq, Hkv, d, r, g)
+    outs = [torch.empty((B, 1, Hq, d), dtype=torch.bfloat16, device="cuda") for _ in kinds]
+    dec.step(token, outs)                       # one plain step first: set-up inside the library happens here
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dec.step(token, outs)
+    t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    t0.record()
+    for i in range(steps):
+        graph.replay()
+        if i % 8 == 7:                          # pairs of beams: both go on from one of the two
+            dec.fork((torch.arange(B, device="cuda") // 2 * 2 + i // 8 % 2).to(torch.int32))
+    t1.record()
+    dec.release(range(0, B, 2))
+    used = int((dec.pages.refs > 0).sum())
+    dec.compact()
+    front = int((dec.pages.refs[:used] > 0).sum())
+    assert lb.lisa_check() == lb.OK and front == used
+    print("%d rows, %d layers: %.1f us a step; %d pages in use after the release, all at the front" %
+          (B, len(kinds), t0.elapsed_time(t1) / steps * 1e3, used))
+
+
+if __name__ == "__main__":
+    main()
