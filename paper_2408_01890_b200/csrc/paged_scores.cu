@@ -535,30 +535,37 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
 
 template <int FMT, int HQ, bool CONCAT>
 cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
-    // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128.  Fewer positions where that
-    // does not give the SMs one and a half (three, and then three quarters, of the concatenating form, whose CTAs take longest).  Eight tenths of the CTAs are taken to have positions (all, where lengths are alike, or six tenths, where they
-    // are spread over [L / 8, L]).
-    constexpr int NW = CONCAT ? 8 : 4;
+    // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128 or 64.  Fewer positions where that
+    // does not give the SMs one CTA and a half (three, and then three quarters, of the concatenating form, whose CTAs take longest), and, where there are KV
+    // heads for them, eight warps to those (7B-shaped, one sequence of 333 11.1 -> 9.8 us, of 2000 17.4 -> 15.2; with 8 KV heads, one of 20000 24.0 and
+    // 25.5).  Eight tenths of the CTAs are taken to have positions (all, where lengths are alike, or six tenths, where they are spread over [L / 8, L]).
     constexpr double fill = 0.8;
     auto ctas = [&](int c) { return fill * p.B * ((p.L + c - 1) / c); };
     int ch = 64;
     if (CONCAT && ctas(128) >= 4 * sm_count()) ch = 128;
     else if (CONCAT && ctas(64) < 3 * sm_count()) ch = 32;
     while (ch > 16 && ctas(ch) < (CONCAT ? 0.75 : 1.5) * sm_count()) ch /= 2;
-    void (*kernel)(ScoresParams, int) = ch == 64 ? paged_scores_kernel<FMT, HQ, NW, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, NW, 32, CONCAT>
-                                                                                               : paged_scores_kernel<FMT, HQ, NW, 16, CONCAT>;
-    if constexpr (CONCAT)
-        if (ch == 128) kernel = paged_scores_kernel<FMT, HQ, NW, 128, CONCAT>;
+    const int NW = CONCAT || (ch < 64 && p.pool.Hkv > 8) ? 8 : 4;
+    void (*kernel)(ScoresParams, int) = ch == 32 ? paged_scores_kernel<FMT, HQ, 8, 32, CONCAT> : paged_scores_kernel<FMT, HQ, 8, 16, CONCAT>;
+    if constexpr (CONCAT) {
+        if (ch == 128) kernel = paged_scores_kernel<FMT, HQ, 8, 128, CONCAT>;
+        if (ch == 64) kernel = paged_scores_kernel<FMT, HQ, 8, 64, CONCAT>;
+    } else if (NW == 4) {
+        kernel = ch == 64 ? paged_scores_kernel<FMT, HQ, 4, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, 4, 32, CONCAT>
+                                                                        : paged_scores_kernel<FMT, HQ, 4, 16, CONCAT>;
+    }
     const size_t smem = (size_t)scores_layout(FMT, HQ, NW, ch, CONCAT, p.m, p.pool.r).total;
     const cudaError_t e = allow_smem(kernel, smem, true);
     if (e != cudaSuccess) return e;
-    // chunks to a CTA: whole waves of as many CTAs as an SM holds (of given lengths six tenths, filling each other's gaps), a CTA's start counted as half a chunk
+    // chunks to a CTA: by the waves of as many CTAs as an SM holds, a CTA's start counted as half a chunk (of given lengths six tenths, of whose waves the last
+    // is on average half empty)
     const int n = (p.L + ch - 1) / ch;
-    const double slots = (CONCAT ? 2. : 4.) * sm_count();
+    const double slots = (NW == 8 ? 2. : 4.) * sm_count();
     int per = 1;
     double least = 1e300;
     for (int q = 1; q <= n && q <= 32; ++q) {
-        const double x = (double)p.B * ((n + q - 1) / q) / slots, cost = (p.seq_lens ? std::max(1., 0.6 * x) : std::ceil(x)) * (2 * q + 1);
+        const double x = (double)p.B * ((n + q - 1) / q) / slots, waves = p.seq_lens ? 0.5 * (0.6 * x + std::ceil(0.6 * x)) : std::ceil(x);
+        const double cost = std::max(1., waves) * (2 * q + 1);
         if (cost < least) { least = cost; per = q; }
     }
     return launch_chained(kernel, dim3((n + per - 1) / per * p.B), dim3(NW * 32), smem, s, p, per);
