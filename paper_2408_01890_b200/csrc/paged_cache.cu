@@ -145,21 +145,15 @@ __device__ __forceinline__ void append_rows_block(const RowsParams& p, const TVi
     float* scale_at = p.pool.scales(page, x.h, x.base) + x.is_v;
     const float held = x.lo > 0 ? *scale_at : 0.f;
     uint32_t amax = 0;
-    if constexpr (sizeof(T) == 2) {                       // two at a time, as unsigned halves
+    // the larger magnitude of two, NaN if one is NaN, in one instruction (whose sign says nothing): bf16 two at a time
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t v = raw[i][e] & 0x7fff7fffu;
-                asm("max.u16x2 %0, %0, %1;" : "+r"(amax) : "r"(v));
-            }
-        amax = max(amax << 16, amax & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) amax = max(amax, raw[i][e] & 0x7fffffffu);
-    }
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(amax) : "r"(raw[i][e]));
+            else asm("max.NaN.xorsign.abs.f32 %0, %0, %1;" : "+r"(amax) : "r"(raw[i][e]));
+        }
+    amax = sizeof(T) == 2 ? max(amax << 16 & 0x7fff0000u, amax & 0x7fff0000u) : amax & 0x7fffffffu;
     const float scale = new_scale<FMT>(amax, held);
     const Encoder<FMT> encode(scale);
     uint8_t* dst = page + (x.is_v ? p.pool.v_off : 0u) + p.pool.row(x.h, x.base) + col;
