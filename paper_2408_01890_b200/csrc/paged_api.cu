@@ -5,7 +5,7 @@
 namespace lisa {
 namespace {
 
-constexpr int kMaxPositions = 1 << 30;   // of a sequence: position arithmetic stays within 32 bits
+constexpr int kMaxPositions = 1 << 29;   // of a sequence: position arithmetic stays within 32 bits
 constexpr int kMaxGrid = 65535;          // sequences are a grid's second or third coordinate
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -40,7 +40,8 @@ lisa_status_t check_step(int B, int Hq, int L, const lisa_paged_layer* c, int ki
     if ((st = check_dims(B, 1, Hq, c->Hkv, c->d)) != LISA_OK) return st;
     if (B > kMaxGrid) return LISA_ERR_UNSUPPORTED;
     if ((st = check_table(t, *c, B)) != LISA_OK) return st;
-    return L < 1 || L > t.max_pages * c->page_tokens ? LISA_ERR_INVALID_ARG : LISA_OK;
+    if (L < 1 || L > t.max_pages * c->page_tokens) return LISA_ERR_INVALID_ARG;
+    return (int64_t)B * ((L + LISA_PAGE_BLOCK - 1) / LISA_PAGE_BLOCK) > INT32_MAX ? LISA_ERR_UNSUPPORTED : LISA_OK;   // (a grid's CTAs)
 }
 
 // A row of scores: fp32 or bf16, aligned to its type; NULL where that is allowed

@@ -342,6 +342,81 @@ def test_shared_attention(fmt, Hq, Hkv, d, r, m, P, integrate, layers, act, w, b
             assert (row[b, :, n:] == 9).all()
 
 
+def check_batch(rng, kind, fmt, Hq, Hkv, P, r, m, lens, integrate=lb.INTEGRATE_ADD, ragged=True, some=None):
+    """A batch through one layer against 64 bits, for the sequences `some` (all when None)."""
+    layer, table, ids = make(rng, kind, fmt, Hkv, P, 128, r, lens)
+    fill(rng, layer, table, lens)
+    mirror = Mirror(layer)
+    B, L = len(lens), max(lens)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda") if ragged else None
+    out, row = torch.empty((B, 1, Hq, 128), device="cuda"), torch.full((B, Hq, L), 9.0, device="cuda")
+    if kind == lb.CACHE_STANDARD:
+        q = normal(rng, B, 1, Hq, 128)
+        lb.lisa_attn_anchor_paged(q.cuda(), layer, table, L=L, seq_lens=seq, out=out, out_scores=row)
+    else:
+        link, prev = make_link(rng, Hq, r, m, B, integrate=integrate), normal(rng, B, Hq, L)
+        lb.lisa_attn_shared_decode_paged(prev.cuda(), link, layer, table, L=L, seq_lens=seq, out=out, out_scores=row)
+    assert lb.lisa_check() == lb.OK
+    for b in range(B) if some is None else some:
+        n = lens[b]
+        if n == 0:
+            assert (out[b] == 0).all() and (row[b] == 9).all()
+            continue
+        K, V = mirror.rows(ids[b], n, 0), mirror.rows(ids[b], n, 1)
+        if kind == lb.CACHE_STANDARD:
+            a = np.einsum("hd,hnd->hn", q[b, 0].double().numpy(), np.repeat(K, Hq // Hkv, 0)) / np.sqrt(128)
+        else:
+            a = shared_scores(prev[b, :, :n].double().numpy(), link.qp[b, 0].double().cpu().numpy(), K, link)
+        close(out[b, 0], softmax_v(a, V, Hq // Hkv), 5e-6, "o of sequence %d" % b)
+        close(row[b, :, :n], a, 1e-6, "row of sequence %d" % b)
+        assert (row[b, :, n:] == 9).all()
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("kind", [lb.CACHE_STANDARD, lb.CACHE_SHARED])
+def test_more_sequences_than_are_dealt(fmt, kind):
+    """150 sequences of lengths 0 .. 200 (up to 128 are numbered on the device), pages of 16."""
+    rng = np.random.default_rng(20)
+    lens = [0, 1, 200] + rng.integers(0, 200, 147).tolist()
+    check_batch(rng, kind, fmt, 32, 4, 16, 21, 64, lens, some=list(range(0, 150, 7)) + [0, 1, 2, 149])
+
+
+@pytest.mark.parametrize("lens", [[0] * 33 + [77] + [0] * 30 + [129], [5] * 128, [0, 0, 0]])
+def test_batches_that_are_mostly_idle_or_all_alike(lens):
+    rng = np.random.default_rng(21)
+    if max(lens) == 0:
+        layer, table, _ = make(rng, lb.CACHE_STANDARD, "s8", 2, 16, 128, 0, [16, 16, 16])
+        out = lb.lisa_attn_anchor_paged(normal(rng, 3, 1, 4, 128).cuda(), layer, table, L=16, seq_lens=torch.zeros(3, dtype=torch.int32, device="cuda"))
+        assert (out == 0).all()
+        return
+    check_batch(rng, lb.CACHE_SHARED, "s8", 32, 8, 16, 21, 64, lens)
+    check_batch(rng, lb.CACHE_STANDARD, "e4m3", 4, 4, 16, 0, 0, lens)
+
+
+@pytest.mark.parametrize("fmt,integrate,r,Hkv", [("s8", lb.INTEGRATE_ADD, 21, 32), ("e4m3", lb.INTEGRATE_ADD, 32, 32), ("e4m3", lb.INTEGRATE_CONCAT, 20, 16),
+                                                 ("s8", lb.INTEGRATE_CONCAT, 25, 16), ("e4m3", lb.INTEGRATE_ADD, 24, 8)])
+@pytest.mark.parametrize("ragged", [True, False])
+def test_many_chunks_to_a_cta(fmt, integrate, r, Hkv, ragged):
+    """64 sequences of 600: several chunks to a CTA of the scores, one after another, and every rank the blocks' layouts distinguish."""
+    rng = np.random.default_rng(22)
+    lens = [600] + (rng.integers(300, 601, 63).tolist() if ragged else [600] * 63)
+    check_batch(rng, lb.CACHE_SHARED, fmt, 32, Hkv, 64, r, 64, lens, integrate, ragged, some=[0, 1, 31, 32, 63])
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("Hq,Hkv", [(16, 8), (3, 1), (5, 1), (6, 6)])
+def test_every_number_of_heads_to_a_kv_head(fmt, Hq, Hkv):
+    rng = np.random.default_rng(Hq)
+    check_batch(rng, lb.CACHE_STANDARD, fmt, Hq, Hkv, 32, 0, 0, [333, 17, 0, 1000])
+
+
+def test_a_long_sequence_over_the_whole_card():
+    """One sequence of 30001 positions: split over wide CTAs, sums of many units."""
+    rng = np.random.default_rng(23)
+    for fmt in FMT:
+        check_batch(rng, lb.CACHE_STANDARD, fmt, 4, 1, 128, 0, 0, [30001], ragged=False)
+
+
 @pytest.mark.parametrize("rows", ["f32", "bf16"])
 def test_a_mask_of_the_lowest_value_in_the_previous_row(rows):
     """The largest finite scores of either sign (a mask in the row of the layer before) stay finite in that layer's own sums: an aligner of zeros there passes
