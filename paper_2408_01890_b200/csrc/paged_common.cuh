@@ -79,32 +79,14 @@ __device__ __forceinline__ uint32_t to_code(float y) {
     }
 }
 
-// The four codes of a word as two pairs of fp16, exactly (s8: 0x6400 | u is 1024 + u, so codes biased by 128 come out as 1152 + code)
-template <int FMT>
-__device__ __forceinline__ uint32_t pair16(uint32_t biased, bool high) {
+// The e4m3 codes in the lower or upper half of a word as a pair of fp16, exactly
+__device__ __forceinline__ uint32_t pair16(uint32_t w, bool high) {
     uint32_t x;
-    if constexpr (FMT == LISA_S8) {
-        x = __byte_perm(biased, 0x64646464u, high ? 0x4342 : 0x4140);
-        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
-        return *reinterpret_cast<const uint32_t*>(&v);
-    } else {
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(x) : "h"((uint16_t)(high ? biased >> 16 : biased)));
-        return x;
-    }
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(x) : "h"((uint16_t)(high ? w >> 16 : w)));
+    return x;
 }
-// The codes in bytes 0 and 2 (or 1 and 3) of a word, likewise
-template <int FMT>
-__device__ __forceinline__ uint32_t across16(uint32_t biased, bool odd) {
-    if constexpr (FMT == LISA_S8) {
-        const uint32_t x = __byte_perm(biased, 0x64646464u, odd ? 0x4341 : 0x4240);
-        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
-        return *reinterpret_cast<const uint32_t*>(&v);
-    } else {
-        return pair16<FMT>(__byte_perm(biased, 0u, odd ? 0x4431 : 0x4420), false);
-    }
-}
-template <int FMT>
-__device__ __forceinline__ uint32_t biased(uint32_t w) { return FMT == LISA_S8 ? w ^ 0x80808080u : w; }
+// Those in bytes 0 and 2 (or 1 and 3)
+__device__ __forceinline__ uint32_t across16(uint32_t w, bool odd) { return pair16(__byte_perm(w, 0u, odd ? 0x4431 : 0x4420), false); }
 
 // A word's code `i` as fp32
 template <int FMT>

@@ -47,9 +47,10 @@ constexpr int kUnit = 2;                                  // tiles that a warp t
 constexpr int kUnitRows = kUnit * kPageBlock;
 constexpr int kBatch = 32 / kUnit;                        // units whose pages the lanes hold
 
-// A stage: K rows (or the given scores [heads][32]), V rows, {K's scale, V's scale} of each tile, whether its page is there
-// WIDE: eight or twelve warps to a CTA instead of four and fewer CTAs to an SM, for grids that leave it at that: a warp takes some 1700 clocks from a
-// unit's scores to its product with V, whatever comes in meanwhile, so a sequence is done sooner by more of them.
+// A stage: K rows (or the given scores [heads][32]), V rows, {K's scale, V's scale} of each tile, whether its page is there.
+// WIDE: eight or twelve warps to a CTA instead of four and fewer CTAs to an SM, for grids of at most one to an SM: a warp takes a unit's scores, maximum,
+// exponentials and product with V one after another whatever comes in meanwhile, so a sequence is done sooner by more warps (2 x 65537 of 8B, as many
+// CTAs either way: 57 us narrow, 54 wide; one of 333 6.7 and 6.2; shape_for has more).
 template <int D, int H, bool GIVEN, bool WIDE>
 struct Stage {
     static constexpr int kFirst = GIVEN ? H * kUnitRows * 4 : kUnitRows * D, kV = kFirst, kScales = kV + kUnitRows * D, kThere = kScales + kUnit * 8;
@@ -134,7 +135,8 @@ __device__ __forceinline__ float query_of(float* x, const AttendParams& p, int b
 
 // The arithmetic of a warp over its units.  Shared memory of a stage: st; pos0: the unit's first position; there: bit u: tile u's page is there.
 //
-// e4m3 with three or more heads to a KV head: products on mma m16n8k16 fp16, where every code is exact; the other operand as two fp16 terms, so that the eight columns are four heads.
+// e4m3 with three or more heads to a KV head: products on mma m16n8k16 fp16, where every code is exact; the other operand as two fp16 terms, so that the eight
+// columns are four heads.
 template <int D, int NT, bool GIVEN>
 struct EngineF16 {
     static constexpr int H = 4 * NT, KW = D / 16, MT = D / 16;   // words of a lane per K row; tiles of 16 output columns
@@ -207,7 +209,7 @@ struct EngineF16 {
                 load_k<D>(kw, st, u);
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
-                    const uint32_t a0 = pair16<LISA_E4M3>(kw[0][w], false), a1 = pair16<LISA_E4M3>(kw[1][w], false), a2 = pair16<LISA_E4M3>(kw[0][w], true), a3 = pair16<LISA_E4M3>(kw[1][w], true);
+                    const uint32_t a0 = pair16(kw[0][w], false), a1 = pair16(kw[1][w], false), a2 = pair16(kw[0][w], true), a3 = pair16(kw[1][w], true);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma_f16(c[nt], a0, a1, a2, a3, qf[nt][w][0], qf[nt][w][1]);
                 }
@@ -293,7 +295,7 @@ struct EngineF16 {
                 load_v<D>(v, st + S::kV, u, c);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const uint32_t a0 = across16<LISA_E4M3>(v[2 * x], false), a1 = across16<LISA_E4M3>(v[2 * x], true), a2 = across16<LISA_E4M3>(v[2 * x + 1], false), a3 = across16<LISA_E4M3>(v[2 * x + 1], true);
+                    const uint32_t a0 = across16(v[2 * x], false), a1 = across16(v[2 * x], true), a2 = across16(v[2 * x + 1], false), a3 = across16(v[2 * x + 1], true);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][c + x], a0, a1, a2, a3, bf[nt][0], bf[nt][1]);
                 }
@@ -508,6 +510,9 @@ struct EngineS8 {
 
 // e4m3 with one or two heads to a KV head: products on mma m16n8k32 e4m3, the codes as they are; the other operand in fixed point as for s8, its 24 bits
 // as six base-16 digits that are codes themselves (Base16) and take six of a head's eight columns.  A lane holds the score of position g + 8 (t % 2) of tile t / 2.
+// Against EngineF16, which turns every code into fp16 for the columns of heads that are not there: given scores, 12 ragged sequences of up to 1901 of the
+// paper's default layer, 39.5 and 42.7 us; 40 x 2900 of 13B 165 and 170; a standard layer 40 x 2900 of 7B, bound by HBM, 148 with both.  With four heads to a KV
+// head (40 x 2900 of 8B) it is the other way round, 203 and 46: twice the accumulators, six eighths of the columns a head.
 template <int D, int NT, bool GIVEN>
 struct EngineE4M3 {
     static constexpr int H = NT, KS = D / 32, MT = D / 16;
@@ -670,7 +675,7 @@ paged_attend_kernel(const __grid_constant__ AttendParams p) {
     chain_release();
     chain_wait();
     int b, split, L;
-    if (!deal_item(p.seq_lens, p.B, p.L, p.tiles * kPageBlock, p.splits, 1, blockIdx.y, b, split, L)) return;
+    if (!work_item(p.seq_lens, p.B, p.L, p.tiles * kPageBlock, blockIdx.y, b, split, L) && (split > 0 || L > 0)) return;
     const int all_tiles = (L + kPageBlock - 1) / kPageBlock;
     const int first = split * p.tiles, end = min(first + p.tiles, all_tiles), parts = (all_tiles + p.tiles - 1) / p.tiles;
     void* out = const_cast<void*>(p.o.ptr);

@@ -114,13 +114,13 @@ struct ScoresLayout {
     int y, qp, q_scale, w1, w2, b1, b2, ring, stage, scales, total;
 };
 // Bytes of a head's q' as operands
-__host__ __device__ constexpr int query_bytes(int fmt) { return fmt == LISA_S8 ? 128 : 192; }
-__host__ __device__ inline ScoresLayout scores_layout(int fmt, int HQ, int NW, int CH, bool concat, int m, int r) {
+constexpr int kQueryBytes = 128;
+__host__ __device__ inline ScoresLayout scores_layout(int HQ, int NW, int CH, bool concat, int m, int r) {
     ScoresLayout l;
     const int HS = NW * 16 / CH, mp = (m + 15) / 16 * 16, kp = concat ? 2 * HQ : (HQ + 15) / 16 * 16;
     int off = HQ * (CH + 4) * 4;
     l.y = off; off += HS > 1 ? HS * HQ * (CH + 4) * 4 : 0;
-    l.qp = off; off += HQ * query_bytes(fmt);
+    l.qp = off; off += HQ * kQueryBytes;
     l.q_scale = off; off += HQ * 4;
     l.w1 = off; off += kp * (mp + 8) * 2;
     l.w2 = off; off += mp * (HQ + 8) * 2;
@@ -135,42 +135,21 @@ __host__ __device__ inline ScoresLayout scores_layout(int fmt, int HQ, int NW, i
 
 // Differences of a KV head's G query heads, whose K' lies in a stage: a block's positions 2g and 2g + 1 are rows g and g + 8 of A, ranks are k.  q: the
 // heads' operands; s_s: their rows of differences.
-//   e4m3  G <= 2: codes as they are, q' as six base-16 digits [6][32] (ranks in the order that A has them), the eight columns being one head;
-//         more: codes as fp16, q' as two fp16 terms [2][32]: column g is head g / 2's leading (even g) or second term
+//   e4m3  codes as fp16, q' as two fp16 terms [2][32]: column g is head g / 2's leading (even g) or second term (for one head to a KV head, six base-16
+//         digits as in paged_decode.cu took longer: 40 x 2900, 13B shape, 165 us, so 161)
 //   s8    codes as they are, q' as three s8 digits [4][32] (the fourth is 0, ranks in the order that A has them): columns 4i .. 4i + 2 are head i's
 template <int FMT, int NB>
 __device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, bool wide, const uint8_t* q, const float* q_scale, int G, float* s_s, int ld) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, ranks = wide ? 32 : 24;
     const float2* sc = reinterpret_cast<const float2*>(stage + scales);
-    constexpr int QB = query_bytes(FMT);
-    if (FMT == LISA_S8 || G <= 2) {
+    if constexpr (FMT == LISA_S8) {
         uint32_t a[NB][4];
 #pragma unroll
         for (int k = 0; k < NB; ++k) {   // (what a block of 24 ranks has behind them: the next block's codes, which meet digits of 0, or zeros)
             uint32_t w[4];
             ldmatrix_trans(w, stage + (k * ranks + lane) * 16);
-            if (FMT != LISA_S8 && !wide) w[3] = 0u;      // (such a code may be NaN)
             a[k][0] = __byte_perm(w[0], w[1], 0x6420); a[k][1] = __byte_perm(w[0], w[1], 0x7531);
             a[k][2] = __byte_perm(w[2], w[3], 0x6420); a[k][3] = __byte_perm(w[2], w[3], 0x7531);
-        }
-        if constexpr (FMT != LISA_S8) {
-            const Base16 base(t);
-            for (int h = 0; h < G; ++h) {
-                const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + h * QB + g * 32) + t;
-                const uint32_t b0 = g < 6 ? qr[0] : 0u, b1 = g < 6 ? qr[4] : 0u;
-                const float qs = q_scale[h];
-                float* to = s_s + h * ld + 2 * g + (t & 1);
-#pragma unroll
-                for (int k = 0; k < NB; k += 2) {        // two blocks at a time (of a chunk of one, twice the same)
-                    const int k1 = NB > 1 ? k + 1 : k;
-                    float c[4] = {0.f, 0.f, 0.f, 0.f}, d[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma_e4m3(c, a[k][0], a[k][1], a[k][2], a[k][3], b0, b1);
-                    mma_e4m3(d, a[k1][0], a[k1][1], a[k1][2], a[k1][3], b0, b1);
-                    const int mine = t & 2 ? k1 : k;
-                    to[mine * kPageBlock] = base.scatter(c, d, t) * (sc[mine].x * qs);
-                }
-            }
-            return;
         }
         if (NB > 1 && G == 1) {          // one head: its digits take the columns of two, with another block each
             const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (g & 3) * 32) + t;
@@ -187,7 +166,7 @@ __device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, b
             return;
         }
         for (int h0 = 0; h0 < G; h0 += 2) {
-            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 2)) * QB + (g & 3) * 32) + t;
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 2)) * kQueryBytes + (g & 3) * 32) + t;
             const bool has = h0 + (g >> 2) < G, mine = h0 + (t >> 1) < G;
             const uint32_t b0 = has ? qr[0] : 0u, b1 = has ? qr[4] : 0u;
             const float qs = mine ? q_scale[h0 + (t >> 1)] : 0.f;
@@ -200,11 +179,10 @@ __device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, b
                 if (mine) to[k * kPageBlock] = x;
             }
         }
-    }
-    if constexpr (FMT != LISA_S8) {
+    } else {
         for (int h0 = 0; h0 < G; h0 += 4) {
             uint32_t bf[4];
-            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 1)) * QB + (g & 1) * 64) + t;
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + (h0 + (g >> 1)) * kQueryBytes + (g & 1) * 64) + t;
             const bool has = h0 + (g >> 1) < G, mine = h0 + t < G;
 #pragma unroll
             for (int i = 0; i < 4; ++i) bf[i] = has && (wide || i < 3) ? qr[4 * i] : 0u;
@@ -214,9 +192,9 @@ __device__ __forceinline__ void delta_blocks(const uint8_t* stage, int scales, b
                 uint32_t w[4];
                 ldmatrix_trans(w, stage + (k * ranks + lane) * 16);
                 float c[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_f16(c, across16<FMT>(w[0], false), across16<FMT>(w[0], true), across16<FMT>(w[1], false), across16<FMT>(w[1], true), bf[0], bf[1]);
-                if (wide) mma_f16(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), across16<FMT>(w[3], false), across16<FMT>(w[3], true), bf[2], bf[3]);
-                else mma_f16_k8(c, across16<FMT>(w[2], false), across16<FMT>(w[2], true), bf[2]);
+                mma_f16(c, across16(w[0], false), across16(w[0], true), across16(w[1], false), across16(w[1], true), bf[0], bf[1]);
+                if (wide) mma_f16(c, across16(w[2], false), across16(w[2], true), across16(w[3], false), across16(w[3], true), bf[2], bf[3]);
+                else mma_f16_k8(c, across16(w[2], false), across16(w[2], true), bf[2]);
                 const float f = sc[k].x * qs;
                 if (mine) *reinterpret_cast<float2*>(s_s + (h0 + t) * ld + k * kPageBlock + 2 * g) = make_float2((c[0] + c[1]) * f, (c[2] + c[3]) * f);
             }
@@ -252,18 +230,12 @@ __device__ __forceinline__ void query_operands(const ScoresParams& p, int b, int
             const int lo = (int)(int8_t)v;
             v = (v - lo) >> 8;
             const int mid = (int)(int8_t)v;
-            uint8_t* at = qp_s + h * query_bytes(FMT) + at_a;
+            uint8_t* at = qp_s + h * kQueryBytes + at_a;
             at[0] = (uint8_t)((v - mid) >> 8); at[32] = (uint8_t)mid; at[64] = (uint8_t)lo; at[96] = 0;
             if (lane == 0) q_scale[h] = amax < INFINITY ? pow2(max(ex - 21, -126)) * rsqrtf((float)r) : __uint_as_float(0x7fc00000u);
-        } else if (p.G <= 2) {
-            const uint32_t v = __float2uint_rn(fabsf(x[i]) * pow2(min(21 - ex, 127))), sign = __float_as_uint(x[i]) >> 24 & 0x80u;    // v <= 2^22
-            uint8_t* at = qp_s + h * query_bytes(FMT) + at_a;
-#pragma unroll
-            for (int q = 0; q < 6; ++q) at[32 * q] = (uint8_t)(sign | (v >> (20 - 4 * q) & 15u));
-            if (lane == 0) q_scale[h] = amax < INFINITY ? pow2(max(ex - 12, -126)) * rsqrtf((float)r) : __uint_as_float(0x7fc00000u);
         } else {
             const float y = x[i] * pow2(13 - ex);
-            __half* at = reinterpret_cast<__half*>(qp_s + h * query_bytes(FMT)) + lane;
+            __half* at = reinterpret_cast<__half*>(qp_s + h * kQueryBytes) + lane;
             const __half hi = __float2half_rn(y);
             at[0] = hi;
             at[32] = __float2half_rn(y - __half2float(hi));
@@ -280,7 +252,7 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     extern __shared__ __align__(16) uint8_t smem_b[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int m = p.m, mp = (m + 15) / 16 * 16, w1_ld = mp + 8, r = p.pool.r;
-    const ScoresLayout lay = scores_layout(FMT, HQ, NW, CH, CONCAT, m, r);
+    const ScoresLayout lay = scores_layout(HQ, NW, CH, CONCAT, m, r);
     float* s_s = reinterpret_cast<float*>(smem_b);
     float* y_s = reinterpret_cast<float*>(smem_b + lay.y);
     uint8_t* qp_s = smem_b + lay.qp;
@@ -308,7 +280,7 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
     __syncwarp();
     chain_wait();
     int b, part, L;
-    if (!deal_item(p.seq_lens, p.B, p.L, per * CH, ((p.L + CH - 1) / CH + per - 1) / per, 0, blockIdx.x, b, part, L)) {
+    if (!work_item(p.seq_lens, p.B, p.L, per * CH, blockIdx.x, b, part, L)) {
         cp_wait<0>();
         return;
     }
@@ -395,7 +367,7 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
             cp_wait<kRingHeads - 2>();
             __syncwarp();
             ask(stage == 0 ? kRingHeads - 1 : stage - 1);
-            delta_blocks<FMT, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + kvh * p.G * query_bytes(FMT), q_scale + kvh * p.G, p.G, s_s + kvh * p.G * LD, LD);
+            delta_blocks<FMT, NB>(ring + stage * lay.stage, lay.scales, r > 24, qp_s + kvh * p.G * kQueryBytes, q_scale + kvh * p.G, p.G, s_s + kvh * p.G * LD, LD);
             stage = stage + 1 == kRingHeads ? 0 : stage + 1;
         }
         if (chunk == 0 && heads == 0) cp_wait<0>();      // (the weights)
@@ -554,7 +526,7 @@ cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
         kernel = ch == 64 ? paged_scores_kernel<FMT, HQ, 4, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, 4, 32, CONCAT>
                                                                         : paged_scores_kernel<FMT, HQ, 4, 16, CONCAT>;
     }
-    const size_t smem = (size_t)scores_layout(FMT, HQ, NW, ch, CONCAT, p.m, p.pool.r).total;
+    const size_t smem = (size_t)scores_layout(HQ, NW, ch, CONCAT, p.m, p.pool.r).total;
     const cudaError_t e = allow_smem(kernel, smem, true);
     if (e != cudaSuccess) return e;
     // chunks to a CTA: by the waves of as many CTAs as an SM holds, a CTA's start counted as half a chunk (of given lengths six tenths, of whose waves the last

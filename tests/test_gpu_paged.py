@@ -374,8 +374,8 @@ def check_batch(rng, kind, fmt, Hq, Hkv, P, r, m, lens, integrate=lb.INTEGRATE_A
 
 @pytest.mark.parametrize("fmt", FMT)
 @pytest.mark.parametrize("kind", [lb.CACHE_STANDARD, lb.CACHE_SHARED])
-def test_more_sequences_than_are_dealt(fmt, kind):
-    """150 sequences of lengths 0 .. 200 (up to 128 are numbered on the device), pages of 16."""
+def test_many_short_sequences(fmt, kind):
+    """150 sequences of lengths 0 .. 200 pages of 16."""
     rng = np.random.default_rng(20)
     lens = [0, 1, 200] + rng.integers(0, 200, 147).tolist()
     check_batch(rng, kind, fmt, 32, 4, 16, 21, 64, lens, some=list(range(0, 150, 7)) + [0, 1, 2, 149])
