@@ -106,7 +106,9 @@ size_t general_smem(const ScoresParams& p) {
 // ---------------------------------------------------------------------------------------------
 // 32 or 40 heads, bf16 weights, hidden widths that are multiples of 8 up to 256, adding or concatenating Integrate
 // ---------------------------------------------------------------------------------------------
-constexpr int kRingHeads = 3;            // KV heads' K' of a warp on their way or in use
+// KV heads' K' of a warp on their way or in use (the concatenating form, whose weights are most of its shared memory, has room for two CTAs an SM with 2: 40 x 1901 of
+// the paper's default layer 120 us, with 3 and one CTA 136)
+__host__ __device__ constexpr int ring_heads(bool concat) { return concat ? 2 : 3; }
 
 // Shared memory of a CTA (byte offsets): differences [HQ][CH + 4], partial FFN outputs [HS][HQ][CH + 4] (HS > 1), q' as operands and its
 // scales, weights, biases, and the warps' rings: a stage is [CH / 16 blocks][24 or 32 ranks][16 positions] and the blocks' scales
@@ -129,7 +131,7 @@ __host__ __device__ inline ScoresLayout scores_layout(int HQ, int NW, int CH, bo
     l.ring = off;
     l.scales = CH / kPageBlock * (r > 24 ? 32 : 24) * 16 + (r > 24 ? 0 : 128);      // (the load of a block of 24 ranks reaches 8 further)
     l.stage = l.scales + (CH / kPageBlock * 8 + 15) / 16 * 16;
-    l.total = off + NW * kRingHeads * l.stage;
+    l.total = off + NW * ring_heads(concat) * l.stage;
     return l;
 }
 
@@ -248,6 +250,7 @@ __device__ __forceinline__ void query_operands(const ScoresParams& p, int b, int
 template <int FMT, int HQ, int NW, int CH, bool CONCAT>
 __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(const __grid_constant__ ScoresParams p, int per) {
     constexpr int THREADS = NW * 32, HS = NW * 16 / CH, LD = CH + 4, NB = CH / kPageBlock, NT2 = HQ / 8, KPH = (HQ + 15) / 16;
+    constexpr int kRingHeads = ring_heads(CONCAT);
     constexpr int KS1 = CONCAT ? 2 * HQ / 16 : KPH, W2_LD = HQ + 8;
     extern __shared__ __align__(16) uint8_t smem_b[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -507,20 +510,18 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 4 : 2) paged_scores_kernel(
 
 template <int FMT, int HQ, bool CONCAT>
 cudaError_t launch_fast(const ScoresParams& p, cudaStream_t s) {
-    // Four warps to 64 positions; the concatenating form, whose weights are most of a CTA's shared memory, eight to 128 or 64.  Fewer positions where that
-    // does not give the SMs one CTA and a half (three, and then three quarters, of the concatenating form, whose CTAs take longest), and, where there are KV
-    // heads for them, eight warps to those (7B-shaped, one sequence of 333 11.1 -> 9.8 us, of 2000 17.4 -> 15.2; with 8 KV heads, one of 20000 24.0 and
+    // 64 positions to four warps (eight of the concatenating form, whose weights are most of a CTA's shared memory; with 128 positions, one CTA to an
+    // SM, 64 x 4000 of the paper's default layer took 361 us, with 64 320).  Fewer positions where that does not give the SMs one CTA and a half (three quarters of
+    // the concatenating form with 32, whose CTAs take longest: 12 ragged of up to 1901 39 us with 32, 36 with 64; 8 of up to 500 16.0 with 32, 14.7 with 16), and, where
+    // there are KV heads for them, eight warps to those (7B-shaped, one sequence of 333 11.1 -> 9.8 us, of 2000 17.4 -> 15.2; with 8 KV heads, one of 20000 24.0 and
     // 25.5).  Eight tenths of the CTAs are taken to have positions (all, where lengths are alike, or six tenths, where they are spread over [L / 8, L]).
     constexpr double fill = 0.8;
     auto ctas = [&](int c) { return fill * p.B * ((p.L + c - 1) / c); };
     int ch = 64;
-    if (CONCAT && ctas(128) >= 4 * sm_count()) ch = 128;
-    else if (CONCAT && ctas(64) < 3 * sm_count()) ch = 32;
-    while (ch > 16 && ctas(ch) < (CONCAT ? 0.75 : 1.5) * sm_count()) ch /= 2;
+    while (ch > 16 && ctas(ch) < (CONCAT && ch == 32 ? 0.75 : 1.5) * sm_count()) ch /= 2;
     const int NW = CONCAT || (ch < 64 && p.pool.Hkv > 8) ? 8 : 4;
     void (*kernel)(ScoresParams, int) = ch == 32 ? paged_scores_kernel<FMT, HQ, 8, 32, CONCAT> : paged_scores_kernel<FMT, HQ, 8, 16, CONCAT>;
     if constexpr (CONCAT) {
-        if (ch == 128) kernel = paged_scores_kernel<FMT, HQ, 8, 128, CONCAT>;
         if (ch == 64) kernel = paged_scores_kernel<FMT, HQ, 8, 64, CONCAT>;
     } else if (NW == 4) {
         kernel = ch == 64 ? paged_scores_kernel<FMT, HQ, 4, 64, CONCAT> : ch == 32 ? paged_scores_kernel<FMT, HQ, 4, 32, CONCAT>
