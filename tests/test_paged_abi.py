@@ -128,6 +128,14 @@ def test_anchor_steps_are_checked(lib, change, status):
     assert lib.lisa_attn_anchor_paged(C.byref(anchor_args(layer(), **change)), None) == status
 
 
+def test_sizes_beyond_the_largest_are_refused(lib):
+    """Sequences of over 2^29 positions, and batches whose blocks of 16 positions are more than a grid has CTAs, before anything is launched."""
+    pages = (1 << 29) // 64
+    for change in (dict(table=table(max_pages=pages + 1, stride=pages + 1)), dict(B=60000, L=1 << 29, table=table(B=60000, max_pages=pages, stride=pages))):
+        assert lib.lisa_attn_anchor_paged(C.byref(anchor_args(layer(), **change)), None) == lb.ERR_UNSUPPORTED
+        assert lib.lisa_attn_shared_decode_paged(C.byref(shared_args(layer(kind=1), **change)), None) == lb.ERR_UNSUPPORTED
+
+
 def shared_args(l, **change):
     a = lb.PagedSharedArgs()
     a.struct_size, a.B, a.Hq, a.L, a.cache, a.table = C.sizeof(lb.PagedSharedArgs), 2, 32, 200, C.pointer(l), table()
