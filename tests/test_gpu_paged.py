@@ -375,7 +375,7 @@ def check_batch(rng, kind, fmt, Hq, Hkv, P, r, m, lens, integrate=lb.INTEGRATE_A
 @pytest.mark.parametrize("fmt", FMT)
 @pytest.mark.parametrize("kind", [lb.CACHE_STANDARD, lb.CACHE_SHARED])
 def test_many_short_sequences(fmt, kind):
-    """150 sequences of lengths 0 .. 200 pages of 16."""
+    """150 sequences of lengths 0 .. 200, pages of 16."""
     rng = np.random.default_rng(20)
     lens = [0, 1, 200] + rng.integers(0, 200, 147).tolist()
     check_batch(rng, kind, fmt, 32, 4, 16, 21, 64, lens, some=list(range(0, 150, 7)) + [0, 1, 2, 149])
@@ -415,6 +415,32 @@ def test_a_long_sequence_over_the_whole_card():
     rng = np.random.default_rng(23)
     for fmt in FMT:
         check_batch(rng, lb.CACHE_STANDARD, fmt, 4, 1, 128, 0, 0, [30001], ragged=False)
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("Hkv", [8, 4, 2, 1])
+@pytest.mark.parametrize("n", [40, 3001])
+def test_masks_in_the_previous_row(fmt, Hkv, n):
+    """A row of -inf where positions are masked, handed on as it is (no aligner): masked positions weigh nothing, wherever they lie; a head with nothing else gives 0;
+    NaN and +inf reach their own head alone."""
+    rng = np.random.default_rng(n + Hkv)
+    layer, table, ids = make(rng, lb.CACHE_SHARED, fmt, Hkv, 32, 64, 8, [n])
+    fill(rng, layer, table, [n])
+    mirror = Mirror(layer)
+    link = make_link(rng, 8, 8, 0, integrate=PLUS)
+    prev, inf = normal(rng, 1, 8, n), float("inf")
+    prev[0, 0] = -inf
+    prev[0, 1, :n - 1] = -inf
+    prev[0, 2, 1:] = -inf
+    prev[0, 3, :n // 2] = -inf
+    prev[0, 4, ::3] = -inf
+    prev[0, 5, n // 3] = float("nan")
+    prev[0, 6, n - 2] = inf
+    out = lb.lisa_attn_shared_decode_paged(prev.cuda(), link, layer, table, L=n, out=torch.empty((1, 1, 8, 64), device="cuda"))[0, 0]
+    a = shared_scores(prev[0].double().numpy(), link.qp[0, 0].double().cpu().numpy(), mirror.rows(ids[0], n, 0), link)
+    assert (out[0] == 0).all() and torch.isnan(out[5]).all() and torch.isnan(out[6]).all()
+    keep, V = [1, 2, 3, 4, 7], np.repeat(mirror.rows(ids[0], n, 1), 8 // Hkv, 0)
+    close(out[keep], softmax_v(a[keep], V[keep], 1), 5e-6, "masked")
 
 
 @pytest.mark.parametrize("rows", ["f32", "bf16"])
